@@ -335,6 +335,88 @@ int mi3d_sgd_update(float *w, const float *dw, void *w_bf16, size_t n, float lr,
 int mi3d_adam_update(float *w, const float *dw, float *m, float *v, void *w_bf16, size_t n, float lr, float beta1,
                      float beta2, float eps, int step, void *stream);
 
+/* ------------------------------------------------------------------------
+ * A residual channel-mixing block over voxels or tokens, y = x + dropout(ffn(layernorm(x))), and its parts on their own.
+ * A "row" is a voxel or a token: tensors are [rows][channels], dense, channel fastest (an NDHWC tensor is one with
+ * N*D*H*W rows).  bf16 unless the name ends in _f32 (the ffn calls take the type from their descriptor); every pointer is
+ * a device pointer, 16-byte aligned unless said otherwise, caller-owned.  Calls only enqueue work on `stream`, on the
+ * current device; they allocate nothing and can be captured into a graph.  Sums are fp32 or wider, results are rounded to
+ * bf16 once, repeated calls give identical bits.  A call with no rows (n = 0, N = 0) is valid and launches nothing but
+ * the zeros of the weights' gradients; its pointers to rows may be null.  Status codes as above.
+ * ---------------------------------------------------------------------- */
+
+/* Layer normalisation of each row over its C channels, with scale gamma and shift beta (C floats each):
+ * xhat = (x - mean) * rstd, rstd = 1 / sqrt(var + eps) with the biased variance, y = gamma * xhat + beta.
+ * stats (may be NULL; 8-byte aligned): (mean, rstd) of each row, 2 * rows floats, for the backward pass.  y may be x.
+ * C <= 16384 in multiples of 8, any other C <= 2048; others and 2^40 rows return MI3D_ERR_UNSUPPORTED. */
+int mi3d_layernorm_fwd(const void *x, const float *gamma, const float *beta, size_t rows, int C, float eps, void *y,
+                       float *stats, void *stream);
+int mi3d_layernorm_fwd_f32(const void *x, const float *gamma, const float *beta, size_t rows, int C, float eps, void *y,
+                           float *stats, void *stream);
+/* Its backward pass from dy, x and stats: with g = dy * gamma,
+ *   dx = rstd * (g - mean_c(g) - xhat * mean_c(g * xhat)) + add,   dgamma = sum over rows of dy * xhat,   dbeta = sum of dy
+ * (C floats each, overwritten, summed in a fixed order).  add (may be NULL): a second gradient of x, such as that of the
+ * connection past the block, of dx's shape.  dx may be dy, x or add.  ws: mi3d_layernorm_workspace_bytes(rows, C) bytes. */
+size_t mi3d_layernorm_workspace_bytes(size_t rows, int C);
+int mi3d_layernorm_bwd(const void *dy, const void *x, const float *stats, const float *gamma, const void *add, size_t rows,
+                       int C, void *dx, float *dgamma, float *dbeta, void *ws, size_t ws_bytes, void *stream);
+int mi3d_layernorm_bwd_f32(const void *dy, const void *x, const float *stats, const float *gamma, const void *add,
+                           size_t rows, int C, void *dx, float *dgamma, float *dbeta, void *ws, size_t ws_bytes,
+                           void *stream);
+
+/* Dropout whose mask is drawn again in the backward pass instead of being stored.  Number i of the stream (seed, offset) is
+ * half i % 2 (0: low) of word (i % 8) / 2 of Philox 4x32-10 (Salmon et al., SC 2011) for the counter words (i / 8 low,
+ * i / 8 high, offset low, offset high) and the key (seed low, seed high).  Value i is kept where number i is below
+ * T = 65536 (1 - p) rounded to a whole number, and then multiplied by 65536 / T; p is thus taken to the next multiple of
+ * 2^-16.  0 <= p <= 1; p = 1 keeps nothing.  A dropped value is 0 whatever it was (an infinity, a NaN).
+ * offset tells the layers and steps of a run apart: streams of different (seed, offset) share no numbers by design.
+ * dev_offset (may be NULL, 8-byte aligned): a number in device memory that is added to offset when the kernel runs, for
+ * captured graphs whose replays have to differ.
+ *   _fwd       out[i] = residual[i] + dropout(a)[i]; residual may be NULL (0); out may be a or residual.
+ *   _bwd       da[i] = dropout(dout)[i] with the same numbers; da may be dout.  (The residual's gradient is dout.)
+ *   _channels  whole feature maps: every value of channel c of sample n of a [N][voxels][C] goes by number n * C + c; forward
+ *              and backward pass alike.  out may be a.  C <= 65536, N <= 65535, voxels < 2^30. */
+int mi3d_dropout_fwd(const void *a, const void *residual, void *out, size_t n, float p, uint64_t seed, uint64_t offset,
+                     const uint64_t *dev_offset, void *stream);
+int mi3d_dropout_fwd_f32(const float *a, const float *residual, float *out, size_t n, float p, uint64_t seed,
+                         uint64_t offset, const uint64_t *dev_offset, void *stream);
+int mi3d_dropout_bwd(const void *dout, void *da, size_t n, float p, uint64_t seed, uint64_t offset,
+                     const uint64_t *dev_offset, void *stream);
+int mi3d_dropout_bwd_f32(const float *dout, float *da, size_t n, float p, uint64_t seed, uint64_t offset,
+                         const uint64_t *dev_offset, void *stream);
+int mi3d_dropout_channels(const void *a, void *out, int N, size_t voxels, int C, float p, uint64_t seed, uint64_t offset,
+                          const uint64_t *dev_offset, void *stream);
+int mi3d_dropout_channels_f32(const float *a, float *out, int N, size_t voxels, int C, float p, uint64_t seed,
+                              uint64_t offset, const uint64_t *dev_offset, void *stream);
+
+/* Gated feed-forward block (two 1x1x1 convolutions, the first with a gate), without biases:
+ *   [g | u] = x w1^T,   h = act(g) * u,   y = h w2^T
+ * x [rows][Cin], w1 [2 F][Cin] (the gate's F rows first), gu [rows][2 F], h [rows][F], w2 [Cout][F], y [rows][Cout], all of
+ * the descriptor's type.  act: MI3D_ACT_SILU, a / (1 + e^-a), or MI3D_ACT_GELU, a Phi(a) with the normal distribution's Phi.
+ * Cin, F and Cout in multiples of 8 up to 65536, rows < 2^31; others return MI3D_ERR_UNSUPPORTED.  Tensors of one call must
+ * not overlap.  ws: mi3d_ffn_workspace_bytes(desc, MI3D_PASS_*) bytes, else MI3D_ERR_WORKSPACE. */
+typedef enum { MI3D_ACT_SILU = 0, MI3D_ACT_GELU = 1 } mi3d_act;
+typedef struct {
+    long long rows;
+    int Cin, F, Cout;
+    int act;   /* mi3d_act */
+    int dtype; /* mi3d_dtype */
+} mi3d_ffn_desc;
+size_t mi3d_ffn_workspace_bytes(const mi3d_ffn_desc *desc, int pass);
+/* The first half: both projections, the activation and the product.  gu may be NULL (inference, or a block that computes it
+ * again in the backward pass with this call).  h is formed from the fp32 sums, gu holds them rounded. */
+int mi3d_ffn_gate(const mi3d_ffn_desc *desc, const void *x, const void *w1, void *h, void *gu, void *stream);
+/* The whole block; h goes through ws.  gu may be NULL. */
+int mi3d_ffn_fwd(const mi3d_ffn_desc *desc, const void *x, const void *w1, const void *w2, void *y, void *gu, void *ws,
+                 size_t ws_bytes, void *stream);
+/* Data gradient from dy and gu: dh = dy w2, dgu = [dh * u * act'(g) | dh * act(g)], h = act(g) * u (again, so that the
+ * forward pass need not keep it), dx = dgu w1.  dgu and h are kept for the weight gradient. */
+int mi3d_ffn_dgrad(const mi3d_ffn_desc *desc, const void *dy, const void *w1, const void *w2, const void *gu, void *dgu,
+                   void *h, void *dx, void *ws, size_t ws_bytes, void *stream);
+/* Weight gradients, fp32, overwritten: dw1 = dgu^T x, dw2 = dy^T h (sums over the rows in a fixed order). */
+int mi3d_ffn_wgrad(const mi3d_ffn_desc *desc, const void *x, const void *dgu, const void *h, const void *dy, float *dw1,
+                   float *dw2, void *ws, size_t ws_bytes, void *stream);
+
 /* ------------------------------------------------------------------------ */
 /* Data-swapping engine                                                     */
 /* ------------------------------------------------------------------------ */

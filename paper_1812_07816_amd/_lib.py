@@ -16,6 +16,10 @@ class View(ctypes.Structure):
     _fields_ = [("pitch", ctypes.c_int), ("offset", ctypes.c_int)]
 
 
+class FfnDesc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_longlong)] + [(k, ctypes.c_int) for k in ("Cin", "F", "Cout", "act", "dtype")]
+
+
 class SwapConfig(ctypes.Structure):
     _fields_ = [("budget_bytes", ctypes.c_size_t), ("dev_arena", ctypes.c_void_p),
                 ("arena_bytes", ctypes.c_size_t), ("host_pool_bytes", ctypes.c_size_t),
@@ -40,6 +44,8 @@ class SwapStats(ctypes.Structure):
 _vp, _sz, _i, _u = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int, ctypes.c_uint
 _pd = ctypes.POINTER(ConvDesc)
 _pi = ctypes.POINTER(ctypes.c_int)
+_pf = ctypes.POINTER(FfnDesc)
+_f, _u64 = ctypes.c_float, ctypes.c_uint64
 
 # name -> (restype, argtypes); one entry per declaration in include/mi3d.h
 SIGNATURES = {
@@ -69,6 +75,22 @@ SIGNATURES = {
     "mi3d_instnorm_lrelu_fwd_f32": (_i, [_vp, _vp, _i, _sz, _i, ctypes.c_float, _vp]),
     "mi3d_instnorm_lrelu_bwd_f32": (_i, [_vp, _vp, _vp, _i, _sz, _i, ctypes.c_float, _vp, _sz, _vp]),
     "mi3d_adam_update": (_i, [_vp, _vp, _vp, _vp, _vp, _sz, ctypes.c_float, ctypes.c_float, ctypes.c_float, ctypes.c_float, _i, _vp]),
+    "mi3d_layernorm_workspace_bytes": (_sz, [_sz, _i]),
+    "mi3d_layernorm_fwd": (_i, [_vp, _vp, _vp, _sz, _i, _f, _vp, _vp, _vp]),
+    "mi3d_layernorm_fwd_f32": (_i, [_vp, _vp, _vp, _sz, _i, _f, _vp, _vp, _vp]),
+    "mi3d_layernorm_bwd": (_i, [_vp, _vp, _vp, _vp, _vp, _sz, _i, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "mi3d_layernorm_bwd_f32": (_i, [_vp, _vp, _vp, _vp, _vp, _sz, _i, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "mi3d_dropout_fwd": (_i, [_vp, _vp, _vp, _sz, _f, _u64, _u64, _vp, _vp]),
+    "mi3d_dropout_fwd_f32": (_i, [_vp, _vp, _vp, _sz, _f, _u64, _u64, _vp, _vp]),
+    "mi3d_dropout_bwd": (_i, [_vp, _vp, _sz, _f, _u64, _u64, _vp, _vp]),
+    "mi3d_dropout_bwd_f32": (_i, [_vp, _vp, _sz, _f, _u64, _u64, _vp, _vp]),
+    "mi3d_dropout_channels": (_i, [_vp, _vp, _i, _sz, _i, _f, _u64, _u64, _vp, _vp]),
+    "mi3d_dropout_channels_f32": (_i, [_vp, _vp, _i, _sz, _i, _f, _u64, _u64, _vp, _vp]),
+    "mi3d_ffn_workspace_bytes": (_sz, [_pf, _i]),
+    "mi3d_ffn_gate": (_i, [_pf, _vp, _vp, _vp, _vp, _vp]),
+    "mi3d_ffn_fwd": (_i, [_pf, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "mi3d_ffn_dgrad": (_i, [_pf, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "mi3d_ffn_wgrad": (_i, [_pf, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
     "mi3d_conv3d_workspace_bytes": (_sz, [_pd, _i]),
     "mi3d_conv3d_fwd": (_i, [_pd, _vp, _vp, _vp, _vp, _sz, _vp]),
     "mi3d_conv3d_dgrad": (_i, [_pd, _vp, _vp, _vp, _vp, _sz, _vp]),

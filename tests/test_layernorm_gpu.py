@@ -1,0 +1,121 @@
+"""Layer normalisation against its formulas in 64 bits: widths that fill the lanes of a row and that do not, odd ones, one row
+and many, statistics far from zero, in place, with a second gradient."""
+import pytest
+import torch
+
+from paper_1812_07816_amd import glue
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+HALF = {torch.bfloat16: 2.0 ** -8, torch.float32: 2.0 ** -24}
+DTYPES = [torch.bfloat16, torch.float32]
+# (rows, C): pieces of eight in 1 to 512 lanes, one value at a time, one row, more rows than one turn of the grid takes
+SHAPES = [(1, 8), (1, 1024), (3, 1), (5, 7), (37, 320), (1000, 32), (70001, 8), (513, 24), (129, 1000), (64, 2048), (33, 4096), (9, 4104), (3, 16384),
+          (65, 333), (17, 2047), (40000, 40), (2, 6400), (300, 257), (20, 12288)]
+
+
+def inputs(rows, C, dtype, mean=0.0, seed=0):
+    gen = torch.Generator().manual_seed(seed + rows * 31 + C)
+    r = lambda *s: torch.randn(*s, generator=gen, dtype=torch.float64)  # noqa: E731
+    x = (r(rows, C) * (0.5 + r(C).abs()) + r(C) * 0.3 + mean).to(dtype)
+    return x, r(rows, C).to(dtype), r(rows, C).to(dtype), (1 + 0.2 * r(C)).float(), (0.2 * r(C)).float()
+
+
+def forward(x, gamma, beta, eps):
+    x, gamma, beta = x.double(), gamma.double(), beta.double()
+    mean = x.mean(1, keepdim=True)
+    rstd = 1 / torch.sqrt((x - mean).square().mean(1, keepdim=True) + eps)
+    return mean, rstd, (x - mean) * rstd
+
+
+def close(got, ref, tol):
+    off = (got.cpu().double() - ref).abs()
+    assert torch.isfinite(got).all()
+    assert (off <= tol).all(), float((off - tol).max())
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=["bf16", "f32"])
+@pytest.mark.parametrize("rows,C", SHAPES)
+def test_forward(device, rows, C, dtype):
+    x, _, _, gamma, beta = inputs(rows, C, dtype, mean=5.0 if C == 1000 else 0.0)
+    eps = 1e-5
+    y, stats = glue.layernorm_fwd(x.to(device), gamma.to(device), beta.to(device), eps=eps)
+    mean, rstd, xhat = forward(x, gamma, beta, eps)
+    xd = x.double().abs()
+    # at most 32 sums in a lane, 9 across the lanes, a product: 64 roundings of a mean; twice that for a mean of squares of differences,
+    # which the error of the mean enters through |x|
+    d_mean = 64 * U * xd.mean(1, keepdim=True)
+    d_rstd = 64 * U + 2 * rstd * (d_mean + U * xd).square().mean(1, keepdim=True).sqrt()
+    close(stats[:, :1], mean, d_mean + 1e-30)
+    close(stats[:, 1:], rstd, rstd * d_rstd)
+    ref = xhat * gamma.double() + beta.double()
+    tol = HALF[dtype] * ref.abs() + gamma.double().abs() * (rstd * (d_mean + 2 * U * xd) + xhat.abs() * (d_rstd + 4 * U)) + 4 * U * beta.double().abs() + 1e-30
+    close(y, ref, tol * 1.01)
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=["bf16", "f32"])
+@pytest.mark.parametrize("rows,C", SHAPES)
+def test_backward(device, rows, C, dtype):
+    x, dy, add, gamma, beta = inputs(rows, C, dtype)
+    mean, rstd, _ = forward(x, gamma, beta, 1e-5)
+    stats = torch.cat([mean, rstd], 1).float()
+    with_add = C % 3 != 0
+    dx, dgamma, dbeta = glue.layernorm_bwd(dy.to(device), x.to(device), stats.to(device), gamma.to(device), add=add.to(device) if with_add else None)
+    m, r = stats[:, :1].double(), stats[:, 1:].double()
+    xd, d = x.double(), dy.double()
+    xhat = (xd - m) * r
+    g = d * gamma.double()
+    a = add.double() if with_add else torch.zeros_like(d)
+    ref = r * (g - g.mean(1, keepdim=True) - xhat * (g * xhat).mean(1, keepdim=True)) + a
+    # xhat carries 2 U (|x| + |m|) r and 2 U; the means 64 roundings of their terms
+    dxh = 2 * U * (xd.abs() + m.abs()) * r + 2 * U * xhat.abs()
+    mg, mgx = g.abs().mean(1, keepdim=True), (g * xhat).abs().mean(1, keepdim=True)
+    tol = r * (8 * U * g.abs() + 64 * U * mg + xhat.abs() * (64 * U * mgx + (g.abs() * dxh).mean(1, keepdim=True)) + (dxh + 8 * U * xhat.abs()) * mgx)
+    close(dx, ref, 1.01 * (HALF[dtype] * ref.abs() + tol + 4 * U * (a.abs() + ref.abs())) + 1e-30)
+    # a lane adds at most rows / 64 + 64 terms in a row here, the lanes of a workgroup 256
+    n = rows / 64 + 320
+    close(dgamma, (d * xhat).sum(0), n * U * (d * xhat).abs().sum(0) + (d.abs() * dxh).sum(0) + 1e-30)
+    close(dbeta, d.sum(0), n * U * d.abs().sum(0) + 1e-30)
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=["bf16", "f32"])
+def test_no_rows_and_in_place(device, dtype):
+    gamma, beta = torch.ones(48, device=device), torch.zeros(48, device=device)
+    e = torch.empty((0, 48), dtype=dtype, device=device)
+    y, stats = glue.layernorm_fwd(e, gamma, beta)
+    assert y.shape == (0, 48) and stats.shape == (0, 2)
+    _, dgamma, dbeta = glue.layernorm_bwd(e, e, stats, gamma, dgamma=torch.full((48,), 7.0, device=device))
+    assert not dgamma.any() and not dbeta.any()
+    x, dy, add, gamma, beta = (t.to(device) for t in inputs(301, 72, dtype))
+    y, stats = glue.layernorm_fwd(x, gamma, beta)
+    dx, dgamma, dbeta = glue.layernorm_bwd(dy, x, stats, gamma, add=add)
+    for where in ("dy", "x", "add"):
+        t = dict(dy=dy.clone(), x=x.clone(), add=add.clone())
+        again = glue.layernorm_bwd(t["dy"], t["x"], stats, gamma, dx=t[where], add=t["add"])
+        assert torch.equal(again[0], dx) and torch.equal(again[1], dgamma) and torch.equal(again[2], dbeta), where
+    z = x.clone()
+    glue.layernorm_fwd(z, gamma, beta, y=z)
+    assert torch.equal(z, y)
+
+
+def test_constant_rows_and_non_finite_rows_stay_apart(device):
+    """A row without variance is beta; an infinity or a NaN spoils its own row and the sums over rows, no other row."""
+    x = torch.randn(70, 96, device=device)
+    x[3] = 2.5
+    gamma, beta = torch.rand(96, device=device), torch.rand(96, device=device)
+    y, stats = glue.layernorm_fwd(x, gamma, beta)
+    assert torch.equal(y[3], beta)
+    bad = x.clone()
+    bad[10, 5], bad[20, 95] = float("inf"), float("nan")
+    yb, _ = glue.layernorm_fwd(bad, gamma, beta)
+    ok = [i for i in range(70) if i not in (10, 20)]
+    assert torch.equal(yb[ok], y[ok]) and not torch.isfinite(yb[20]).any()
+
+
+def test_rows_behind_the_last_stay_as_they_are(device):
+    x, dy, _, gamma, beta = (t.to(device) for t in inputs(130, 40, torch.bfloat16))
+    y, st, dx = (torch.full(s, 9.0, dtype=d, device=device) for s, d in (((130, 40), torch.bfloat16), ((130, 2), torch.float32), ((130, 40), torch.bfloat16)))
+    glue.layernorm_fwd(x[:67], gamma, beta, y=y[:67], stats=st[:67])
+    glue.layernorm_bwd(dy[:67], x[:67], st[:67], gamma, dx=dx[:67])
+    assert (y[67:] == 9).all() and (st[67:] == 9).all() and (dx[67:] == 9).all() and not (dx[:67] == 9).all()
