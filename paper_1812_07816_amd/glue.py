@@ -132,19 +132,26 @@ def instnorm_lrelu_bwd(da, a, stats, ws, slope=0.01):
     check(fn(_p(da), _p(a), _p(stats), N, a.numel() // (N * C), C, slope, _p(ws), ws.numel(), _stream()), "instnorm_lrelu_bwd")
 
 
-def _operands(dtype, shape, **tensors):
-    """Refuses what is not a dense tensor of this type and shape on the current device (None: left out)."""
-    dev = torch.cuda.current_device() if torch.cuda.is_available() else None
+def _current(t, name):
+    """The current stream of the current device, where t has to be (half a microsecond; a torch stream object takes three)."""
+    dev = t.get_device()
+    if dev < 0 or dev != torch.cuda.current_device():
+        raise ValueError(f"{name}: need a tensor on the current device, got one on {t.device}")
+    return dev, torch._C._cuda_getCurrentRawStream(dev)
+
+
+def _operands(dev, dtype, shape, **tensors):
+    """Refuses what is not a dense tensor of this type and shape on this device (None: left out)."""
     for name, t in tensors.items():
-        if t is not None and (t.get_device() != dev or t.dtype != dtype or t.shape != shape or not t.is_contiguous()):
+        if t is not None and (t.get_device() != dev or t.dtype is not dtype or t.shape != shape or not t.is_contiguous()):
             raise ValueError(f"{name}: need contiguous {dtype} tensor of shape {tuple(shape)} on the current device, got {t.dtype} {tuple(t.shape)} on {t.device}")
 
 
 def _typed(name, dtype):
-    if dtype == torch.float32:
-        return getattr(lib(), name + "_f32")
-    if dtype == torch.bfloat16:
+    if dtype is torch.bfloat16:
         return getattr(lib(), name)
+    if dtype is torch.float32:
+        return getattr(lib(), name + "_f32")
     raise ValueError(f"{name[5:]}: bf16 and fp32 tensors, got {dtype}")
 
 
@@ -159,22 +166,24 @@ def layernorm_workspace(rows, C):
 def layernorm_fwd(x, gamma, beta, y=None, stats=None, eps=IN_EPS):
     """y = gamma * (x - mean) * rstd + beta over the last dimension of x, stats[row] = (mean, rstd); gamma, beta and stats fp32.
     y may be x."""
-    fn, shape, C = _typed("mi3d_layernorm_fwd", x.dtype), x.shape, x.shape[-1]
+    fn, shape, C, dt = _typed("mi3d_layernorm_fwd", x.dtype), x.shape, x.shape[-1], torch.float32
+    dev, stream = _current(x, "x")
     rows = x.numel() // max(C, 1)
     if y is None:
         y = torch.empty_like(x, memory_format=torch.contiguous_format)
     if stats is None:
         stats = torch.empty((rows, 2), dtype=torch.float32, device=x.device)
-    _operands(x.dtype, shape, x=x, y=y)
-    _operands(torch.float32, (C,), gamma=gamma, beta=beta)
-    _operands(torch.float32, (rows, 2), stats=stats)
-    check(fn(x.data_ptr(), gamma.data_ptr(), beta.data_ptr(), rows, C, eps, y.data_ptr(), stats.data_ptr(), _stream()), "layernorm_fwd")
+    _operands(dev, x.dtype, shape, x=x, y=y)
+    _operands(dev, dt, (C,), gamma=gamma, beta=beta)
+    _operands(dev, dt, (rows, 2), stats=stats)
+    check(fn(x.data_ptr(), gamma.data_ptr(), beta.data_ptr(), rows, C, eps, y.data_ptr(), stats.data_ptr(), stream), "layernorm_fwd")
     return y, stats
 
 
 def layernorm_bwd(dy, x, stats, gamma, dx=None, dgamma=None, dbeta=None, ws=None, add=None):
     """dx (+ add, the gradient of a connection past the block), dgamma, dbeta.  dx may be dy, x or add."""
-    fn, shape, C = _typed("mi3d_layernorm_bwd", x.dtype), x.shape, x.shape[-1]
+    fn, shape, C, dt = _typed("mi3d_layernorm_bwd", x.dtype), x.shape, x.shape[-1], torch.float32
+    dev, stream = _current(x, "x")
     rows = x.numel() // max(C, 1)
     if dx is None:
         dx = torch.empty_like(x, memory_format=torch.contiguous_format)
@@ -182,52 +191,49 @@ def layernorm_bwd(dy, x, stats, gamma, dx=None, dgamma=None, dbeta=None, ws=None
         dgamma = torch.empty(C, dtype=torch.float32, device=x.device)
     if dbeta is None:
         dbeta = torch.empty(C, dtype=torch.float32, device=x.device)
-    _operands(x.dtype, shape, dy=dy, x=x, dx=dx, add=add)
-    _operands(torch.float32, (C,), gamma=gamma, dgamma=dgamma, dbeta=dbeta)
-    _operands(torch.float32, (rows, 2), stats=stats)
+    _operands(dev, x.dtype, shape, dy=dy, x=x, dx=dx, add=add)
+    _operands(dev, dt, (C,), gamma=gamma, dgamma=dgamma, dbeta=dbeta)
+    _operands(dev, dt, (rows, 2), stats=stats)
     if ws is None:
         ws = layernorm_workspace(rows, C)
-    _operands(torch.uint8, ws.shape, ws=ws)
+    _operands(dev, torch.uint8, ws.shape, ws=ws)
     check(fn(dy.data_ptr(), x.data_ptr(), stats.data_ptr(), gamma.data_ptr(), _ptr(add), rows, C, dx.data_ptr(), dgamma.data_ptr(), dbeta.data_ptr(),
-             ws.data_ptr(), ws.numel(), _stream()), "layernorm_bwd")
+             ws.data_ptr(), ws.numel(), stream), "layernorm_bwd")
     return dx, dgamma, dbeta
-
-
-def _dev_offset(t):
-    if t is not None:
-        _operands(torch.int64, (1,), dev_offset=t)
-    return _ptr(t)
 
 
 def dropout_fwd(a, p, seed, offset=0, residual=None, out=None, dev_offset=None):
     """out = residual + dropout(a) with the numbers of stream (seed, offset); dev_offset: an int64 of one value on the device that is
     added to offset when the kernel runs.  out may be a or residual."""
-    fn = _typed("mi3d_dropout_fwd", a.dtype)
+    fn, (dev, stream) = _typed("mi3d_dropout_fwd", a.dtype), _current(a, "a")
     if out is None:
         out = torch.empty_like(a, memory_format=torch.contiguous_format)
-    _operands(a.dtype, a.shape, a=a, residual=residual, out=out)
-    check(fn(a.data_ptr(), _ptr(residual), out.data_ptr(), a.numel(), p, seed, offset, _dev_offset(dev_offset), _stream()), "dropout_fwd")
+    _operands(dev, a.dtype, a.shape, a=a, residual=residual, out=out)
+    _operands(dev, torch.int64, (1,), dev_offset=dev_offset)
+    check(fn(a.data_ptr(), _ptr(residual), out.data_ptr(), a.numel(), p, seed, offset, _ptr(dev_offset), stream), "dropout_fwd")
     return out
 
 
 def dropout_bwd(dout, p, seed, offset=0, da=None, dev_offset=None):
     """da = the gradient of dropout_fwd's a: the same values are dropped.  da may be dout."""
-    fn = _typed("mi3d_dropout_bwd", dout.dtype)
+    fn, (dev, stream) = _typed("mi3d_dropout_bwd", dout.dtype), _current(dout, "dout")
     if da is None:
         da = torch.empty_like(dout, memory_format=torch.contiguous_format)
-    _operands(dout.dtype, dout.shape, dout=dout, da=da)
-    check(fn(dout.data_ptr(), da.data_ptr(), dout.numel(), p, seed, offset, _dev_offset(dev_offset), _stream()), "dropout_bwd")
+    _operands(dev, dout.dtype, dout.shape, dout=dout, da=da)
+    _operands(dev, torch.int64, (1,), dev_offset=dev_offset)
+    check(fn(dout.data_ptr(), da.data_ptr(), dout.numel(), p, seed, offset, _ptr(dev_offset), stream), "dropout_bwd")
     return da
 
 
 def dropout_channels(a, p, seed, offset=0, out=None, dev_offset=None):
     """Drops whole channels of the samples of a [N, ..., C]; forward and backward pass alike.  out may be a."""
-    fn = _typed("mi3d_dropout_channels", a.dtype)
     if a.dim() < 2:
         raise ValueError(f"a: need [N, ..., C], got {tuple(a.shape)}")
+    fn, (dev, stream) = _typed("mi3d_dropout_channels", a.dtype), _current(a, "a")
     if out is None:
         out = torch.empty_like(a, memory_format=torch.contiguous_format)
-    _operands(a.dtype, a.shape, a=a, out=out)
+    _operands(dev, a.dtype, a.shape, a=a, out=out)
+    _operands(dev, torch.int64, (1,), dev_offset=dev_offset)
     N, C = a.shape[0], a.shape[-1]
-    check(fn(a.data_ptr(), out.data_ptr(), N, a.numel() // max(N * C, 1), C, p, seed, offset, _dev_offset(dev_offset), _stream()), "dropout_channels")
+    check(fn(a.data_ptr(), out.data_ptr(), N, a.numel() // max(N * C, 1), C, p, seed, offset, _ptr(dev_offset), stream), "dropout_channels")
     return out
