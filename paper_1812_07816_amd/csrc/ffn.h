@@ -1,0 +1,45 @@
+// What the kernels of the gated feed-forward block share.
+#pragma once
+#include "mi3d_internal.h"
+#include "rows_common.h"
+
+namespace mi3d {
+
+// act(g) and act'(g); silu: g s(g) with the logistic s, gelu: g Phi(g) with the normal distribution's Phi.  bf16: the hardware's
+// exponential and reciprocal, and Phi from the rational approximation 7.1.26 of Abramowitz and Stegun's Handbook (error
+// of erf below 1.5e-7), whose exponential is that of the derivative as well; fp32: the library's functions.
+template <typename T>
+__device__ __forceinline__ void activation(float g, int act, float& a, float& d) {
+    if (act == MI3D_ACT_SILU) {
+        const float s = sizeof(T) == 2 ? __builtin_amdgcn_rcpf(1.f + __expf(-g)) : 1.f / (1.f + expf(-g));
+        a = g * s;
+        d = fmaf(a, 1.f - s, s);
+    } else {
+        const float e = sizeof(T) == 2 ? __expf(-0.5f * g * g) : expf(-0.5f * g * g);      // e^(-z^2), z = |g| / sqrt 2
+        float c;
+        if (sizeof(T) == 2) {
+            const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678f, fabsf(g), 1.f));
+            const float q = 0.5f * e * t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+            c = g < 0.f ? q : 1.f - q;
+        } else {
+            c = 0.5f * (1.f + erff(g * 0.70710678f));
+        }
+        a = g * c;
+        d = fmaf(g * 0.39894228f, e, c);
+    }
+}
+template <typename T>
+__device__ __forceinline__ float activation(float g, int act) {
+    float a, d;
+    activation<T>(g, act, a, d);
+    return a;
+}
+
+
+// The forward products of few rows, or of small matrices.  gated: w holds 2 N rows, out = act(g) * u (and [g | u] where gu is not
+// null); otherwise N rows and out = x w^T.  K and N are multiples of 8.  few_rows_us: what its model expects it to take (very long:
+// too many rows).
+double few_rows_us(bool bf16, bool gated, long long rows, long long K, long long N);
+int few_rows_product(bool bf16, bool gated, const void* x, const void* w, long long rows, int K, int N, int act, void* out, void* gu, hipStream_t s);
+
+}  // namespace mi3d

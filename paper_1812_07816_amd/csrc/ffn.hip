@@ -9,11 +9,9 @@
 // (bf16: ds_read_b64_tr_b16), so that no pass rewrites a tensor or the weights.  P goes into the first operand of the matrix
 // instruction, whose results a lane then holds as four neighbouring n of one row.  bf16: v_mfma_f32_32x32x16_bf16; fp32:
 // v_mfma_f32_32x32x2_f32 on the same 16-byte pieces, four of k.  Sums in fp32.  Bound: the matrix instructions.
-#include <cmath>
 
+#include "ffn.h"
 #include "ig_common.h"
-#include "mi3d_internal.h"
-#include "rows_common.h"
 
 namespace mi3d {
 namespace {
@@ -41,56 +39,31 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const char* p, long lon
     return __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, bytes > 0x7fffffffll ? 0x7fffffff : bytes < 0 ? 0 : (int)bytes, 0x00020000);
 }
 
-// act(g) and act'(g); silu: g s(g) with the logistic s, gelu: g Phi(g) with the normal distribution's Phi
-__device__ __forceinline__ float activation(float g, int act) {
-    if (act == MI3D_ACT_SILU) return g / (1.f + expf(-g));
-    return 0.5f * g * (1.f + erff(g * 0.70710678f));
-}
-__device__ __forceinline__ void activation(float g, int act, float& a, float& d) {
-    if (act == MI3D_ACT_SILU) {
-        const float s = 1.f / (1.f + expf(-g));
-        a = g * s;
-        d = s * (1.f + g * (1.f - s));
-    } else {
-        const float c = 0.5f * (1.f + erff(g * 0.70710678f));
-        a = g * c;
-        d = c + g * 0.39894228f * expf(-0.5f * g * g);
-    }
-}
+// eight values as they lie in memory
+template <typename T> struct Eight;
+template <> struct Eight<uint16_t> {
+    uint4 v;
+    __device__ __forceinline__ void unpack(float (&f)[8]) const { load_values<uint16_t, 8>((const uint16_t*)&v, f); }
+};
+template <> struct Eight<float> {
+    float4 v[2];
+    __device__ __forceinline__ void unpack(float (&f)[8]) const { load_values<float, 8>((const float*)v, f); }
+};
 
-template <typename T>
-__device__ __forceinline__ void load4(const T* p, float (&f)[4]) {
-    if constexpr (sizeof(T) == 2) {
-        const uint2 v = *(const uint2*)p;
-        f[0] = __builtin_bit_cast(float, v.x << 16);
-        f[1] = __builtin_bit_cast(float, v.x & 0xFFFF0000u);
-        f[2] = __builtin_bit_cast(float, v.y << 16);
-        f[3] = __builtin_bit_cast(float, v.y & 0xFFFF0000u);
-    } else {
-        const float4 v = *(const float4*)p;
-        f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w;
-    }
-}
-template <typename T>
-__device__ __forceinline__ void store4(T* p, const float (&f)[4]) {
-    if constexpr (sizeof(T) == 2) *(uint2*)p = uint2{pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3])};
-    else *(float4*)p = float4{f[0], f[1], f[2], f[3]};
-}
-
-// One operand's share of a step in LDS: R rows of 128 bytes of k (ACROSS false), or 128 / sizeof(T) rows of k of R values.  16-byte
+// One operand's share of a step in LDS: R rows of KB bytes of k (ACROSS false), or KB / sizeof(T) rows of k of R values.  16-byte
 // pieces are permuted inside a row so that the lanes of a read fall into different banks.
-template <typename T, int R, bool ACROSS>
+template <typename T, int R, int KB, bool ACROSS>
 struct Operand {
-    static constexpr int E = sizeof(T), KS = 128 / E, ROW = ACROSS ? R * E : 128, PER = ROW / 16;    // bytes, pieces of a row
+    static constexpr int E = sizeof(T), ROW = ACROSS ? R * E : KB, PER = ROW / 16;    // bytes, pieces of a row
     static __device__ __forceinline__ int swizzle(int row) {
-        if (!ACROSS) return row & 7;
+        if (!ACROSS) return KB == 128 ? row >> 1 & 7 : row >> 2 & 3;      // (sixteen rows fill the 256 bytes of the banks)
         if (E == 4) return 2 * (row & 4);
         return ROW >= 256 ? 4 * (row & 3) : 2 * (row & 2);
     }
-    // fragments of the block of 32 that begins at `at`, of the kk-th sixteen (fp32: eight) k of the step
+    // fragments of the block of 32 that begins at `at` (a multiple of 32)
     static __device__ __forceinline__ int place(int at, int lane) {
         const int ln = lane & 31, half = lane >> 5;
-        if (!ACROSS) return (at + ln) * 128;      // (the piece depends on kk)
+        if (!ACROSS) return (at + ln) * KB;      // (the piece depends on kk)
         if (E == 4) return 4 * half * ROW + ((((at + ln) >> 2) ^ (8 * half)) << 4) + (ln & 3) * 4;
         const int g = lane >> 4, row = 8 * (g >> 1) + (lane >> 2 & 3), c8 = lane & 3;
         return row * ROW + ((((at + 16 * (g & 1)) / 8 + (c8 >> 1)) ^ swizzle(row)) << 4) + (c8 & 1) * 8;
@@ -99,10 +72,11 @@ struct Operand {
         bf16x8 h;
         float f[4];
     };
+    // of the kk-th sixteen (fp32: eight) k of the step
     static __device__ __forceinline__ Frag read(const char* l, int place, int kk, int lane) {
         Frag r;
         if constexpr (!ACROSS) {
-            const char* p = l + place + (((2 * kk + (lane >> 5)) ^ (lane & 7)) << 4);      // (blocks begin at multiples of 32)
+            const char* p = l + place + (((2 * kk + (lane >> 5)) ^ swizzle(lane & 31)) << 4);
             if constexpr (E == 2) r.h = *(const bf16x8*)p;
             else {
                 const float4 v = *(const float4*)p;
@@ -119,13 +93,14 @@ struct Operand {
 };
 
 // A workgroup of WM x WN waves owns 32 MB WM rows x 64 WN columns of D (GATE: columns of g and of u, half each); a wave MB x 2 blocks of
-// 32 x 32.  Two stages of LDS: a step's loads run while the step before is computed.
-template <typename T, int MB, int WM, int WN, bool QA, bool PA, Form FORM>
+// 32 x 32.  A step is KB bytes of k; RING steps have a place in LDS, RING - 1 are under way while one is computed.
+template <typename T, int MB, int WM, int WN, int KB, int RING, bool QA, bool PA, Form FORM>
 __global__ void __launch_bounds__(64 * WM * WN, 2) ffn_gemm_kernel(const FfnParams P) {
-    constexpr int W = WM * WN, BM = 32 * MB * WM, BN = 64 * WN, E = sizeof(T), KS = 128 / E;
-    constexpr int NQ = BM / (8 * W), NP = BN / (8 * W), Q_BYTES = BM * 128, STAGE = (BM + BN) * 128;
-    typedef Operand<T, BM, QA> OQ;
-    typedef Operand<T, BN, PA> OP;
+    constexpr int W = WM * WN, BM = 32 * MB * WM, BN = 64 * WN, E = sizeof(T), KS = KB / E;
+    constexpr int NQ = BM * KB / 1024 / W, NP = BN * KB / 1024 / W, Q_BYTES = BM * KB, STAGE = (BM + BN) * KB;
+    constexpr int ROWS = 1024 / KB;      // (k along) rows of a wave's load
+    typedef Operand<T, BM, KB, QA> OQ;
+    typedef Operand<T, BN, KB, PA> OP;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
 
@@ -147,15 +122,16 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) ffn_gemm_kernel(const FfnPara
     const long long qrow = (long long)P.qp * E, prow = (long long)P.pp * E;
     // byte offsets of the pieces this lane fetches in the buffers below
     unsigned qo[NQ], po[NP];
-    const int kq = ((lane & 7) ^ (lane >> 3)) * 16;      // (k along: byte of k inside a step)
+    const int rl = lane / (KB / 16), kq = ((lane % (KB / 16)) ^ Operand<T, BM, KB, false>::swizzle(ROWS * (wave & 1) + rl)) * 16;      // (k along) row of the load, byte of k inside a step
 #pragma unroll
     for (int i = 0; i < NQ; ++i) {
         const int g = i * W + wave;
         if constexpr (QA) {
             const int row = g * 64 / OQ::PER + lane / OQ::PER;
             qo[i] = (unsigned)(row * qrow + ((lane % OQ::PER) ^ OQ::swizzle(row)) * 16);
-        } else qo[i] = (unsigned)((8 * g + (lane >> 3)) * qrow + kq);
+        } else qo[i] = (unsigned)((ROWS * g + rl) * qrow + kq);
     }
+    auto up = [&](int i) { return FORM == GATE && (ROWS * (i * W + wave) & 32); };      // GATE: 32 rows of the gate, the same 32 of up, ...
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
         const int g = i * W + wave;
@@ -163,30 +139,32 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) ffn_gemm_kernel(const FfnPara
             const int row = g * 64 / OP::PER + lane / OP::PER;
             po[i] = (unsigned)(row * prow + ((lane % OP::PER) ^ OP::swizzle(row)) * 16);
         } else {
-            // GATE: 32 rows of the gate, the same 32 of up, ...
-            const int row = FORM == GATE ? 32 * (g >> 3) + 8 * (g & 3) : 8 * g;
-            po[i] = (unsigned)((row + (lane >> 3)) * prow + kq);
+            const int row = FORM == GATE ? 32 * (ROWS * g / 64) + ROWS * g % 32 : ROWS * g;
+            po[i] = (unsigned)((row + rl) * prow + kq);
         }
     }
     const unsigned lds_wave = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(lds_char)lds) + wave * 1024;
     const char *q = (const char*)P.q, *p = (const char*)P.p;
-    auto fetch = [&](long long s) {
-        const unsigned l = lds_wave + (unsigned)((s - s0) & 1) * STAGE;
-        const long long k = s * 128;                     // (k along) byte of k
-        {
-            const long long at = QA ? s * KS * qrow + m0 * E : m0 * qrow;
-            const __amdgpu_buffer_rsrc_t r = buffer(q + at, (QA ? P.K : P.M) * qrow - at);
-#pragma unroll
-            for (int i = 0; i < NQ; ++i)
-                load_lds_asm(r, l + i * W * 1024, QA ? qo[i] : k + kq < kbytes ? qo[i] + (unsigned)k : OOB);
-        }
-        const long long at = PA ? s * KS * prow + (long long)n0 * E : n0 * prow;
+    // The step under way to LDS: its place and buffers (of no bytes behind the last step: loads that write zeros where nobody reads)
+    unsigned slot_in = 0, to = 0;
+    bool inside = false;                                 // (k along) this lane's piece lies before the end of k
+    __amdgpu_buffer_rsrc_t rq = buffer(q, 0), rp = rq, ru = rq;
+    auto begin = [&](long long s) {
+        to = lds_wave + slot_in * STAGE;
+        slot_in = slot_in + 1 == RING ? 0 : slot_in + 1;
+        const long long k = s * KB, none = s < s1 ? 0 : 1ll << 62;
+        inside = k + kq < kbytes;
+        const long long aq = QA ? s * KS * qrow + m0 * E : m0 * qrow + k;
+        rq = buffer(q + aq, (QA ? P.K : P.M) * qrow - aq - none);
+        const long long ap = PA ? s * KS * prow + (long long)n0 * E : n0 * prow + k;
         const long long all = PA ? P.K * prow : (FORM == GATE ? P.F : P.N) * prow;
-        const __amdgpu_buffer_rsrc_t r = buffer(p + at, all - at);
-        const __amdgpu_buffer_rsrc_t r2 = buffer(p + at + (FORM == GATE ? all : 0), all - at);
-#pragma unroll
-        for (int i = 0; i < NP; ++i)
-            load_lds_asm(FORM == GATE && (i * W + wave) & 4 ? r2 : r, l + Q_BYTES + i * W * 1024, PA ? po[i] : k + kq < kbytes ? po[i] + (unsigned)k : OOB);
+        rp = buffer(p + ap, all - ap - none);
+        if (FORM == GATE) ru = buffer(p + ap + all, all - ap - none);
+    };
+    constexpr int NL = NQ + NP;
+    auto load = [&](int i) {
+        if (i < NQ) load_lds_asm(rq, to + i * W * 1024, QA || inside ? qo[i] : OOB);
+        else load_lds_asm(up(i - NQ) ? ru : rp, to + Q_BYTES + (i - NQ) * W * 1024, PA || inside ? po[i - NQ] : OOB);
     };
 
     f32x16 acc[MB][2];
@@ -204,99 +182,175 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) ffn_gemm_kernel(const FfnPara
 #pragma unroll
     for (int b = 0; b < 2; ++b) fp[b] = Q_BYTES + OP::place(wn + 32 * b, lane);
 
-    if (s0 < s1) fetch(s0);
+    // A step is KK turns of sixteen (fp32: eight) k.  Between a turn's products stand the reads of the next turn's fragments and a
+    // share of a step's loads, so that no wave stands in line for LDS or the address unit while its matrix unit idles; before the last
+    // turn's stands the barrier behind which the next step is read and this step's place filled.
+    constexpr int KK = KB / 32, NR = MB + 2, NM = 2 * MB;
+    typename OQ::Frag vq[2][MB];
+    typename OP::Frag vp[2][2];
+    auto read = [&](const char* l, int kk, int to, int j) {      // in the order of the products
+        if (j == 0 || j == 2) vp[to][j / 2] = OP::read(l, fp[j / 2], kk, lane);
+        else vq[to][j == 1 ? 0 : j - 2] = OQ::read(l, fq[j == 1 ? 0 : j - 2], kk, lane);
+    };
+    if (s0 < s1) {
+#pragma unroll
+        for (int i = 0; i < RING; ++i) {
+            begin(s0 + i);
+#pragma unroll
+            for (int j = 0; j < NL; ++j)
+                if (i < RING - 1 || j < NL / KK) load(j);      // (the rest of the last one in the first step's turns)
+        }
+        asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((RING - 2) * NL + NL / KK) : "memory");
+#pragma unroll
+        for (int j = 0; j < NR; ++j) read(lds, 0, 0, j);
+    }
+    const char* l = lds;
+    unsigned slot = 0;
     for (long long s = s0; s < s1; ++s) {
-        // this step's pieces have come, in all waves, and all have read the step before
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        if (s + 1 < s1) fetch(s + 1);
-        const char* l = lds + ((s - s0) & 1) * STAGE;
 #pragma unroll
-        for (int kk = 0; kk < 4; ++kk) {
-            typename OQ::Frag vq[MB];
-            typename OP::Frag vp[2];
+        for (int kk = 0; kk < KK; ++kk) {
+            if (kk == KK - 1) {
+                // the next step's pieces have come (those of the RING - 2 behind it may be under way), in all waves, and all have read this step
+                asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((RING - 2) * NL) : "memory");
+                begin(s + RING);
+                slot = slot + 1 == RING ? 0 : slot + 1;
+                l = lds + slot * STAGE;
+            }
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int a = 0; a < MB; ++a) vq[a] = OQ::read(l, fq[a], kk, lane);
+            for (int m = 0; m < NM; ++m) {
+                const int a = m / 2, b = m % 2;
+                const typename OP::Frag& x = vp[kk & 1][b];
+                const typename OQ::Frag& y = vq[kk & 1][a];
+                if constexpr (E == 2) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x.h, y.h, acc[a][b], 0, 0, 0);
+                else
 #pragma unroll
-            for (int b = 0; b < 2; ++b) vp[b] = OP::read(l, fp[b], kk, lane);
+                    for (int j = 0; j < 4; ++j) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x2f32(x.f[j], y.f[j], acc[a][b], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int a = 0; a < MB; ++a)
+                for (int j = 0; j < NR; ++j)
+                    if (j * NM / NR == m) read(l, kk < KK - 1 ? kk + 1 : 0, (kk + 1) & 1, j);
+                const int part = kk == KK - 1 ? 0 : kk + 1;      // of the step's loads
 #pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    if constexpr (E == 2) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vp[b].h, vq[a].h, acc[a][b], 0, 0, 0);
-                    else
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x2f32(vp[b].f[j], vq[a].f[j], acc[a][b], 0, 0, 0);
-                }
+                for (int j = NL * part / KK; j < NL * (part + 1) / KK; ++j)
+                    if ((j - NL * part / KK) * NM / (NL * (part + 1) / KK - NL * part / KK) == m) load(j);
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // (the loads behind the last step)
 
-    // lane (row ln, half): registers 4 i .. 4 i + 3 of a block are columns 8 i + 4 half .. + 3 of its 32
-    const int ln = lane & 31, half = lane >> 5;
+    // The results go through LDS (a lane holds four columns of one row; 16-byte pieces permuted by the row) so that each row's are
+    // read and written in whole lines, eight values a thread, RA of the MB blocks of rows at a time.  The data gradient's g and u
+    // are requested before.
+    constexpr int BLOCKS = RING * STAGE / (32 * WM * BN * 4), RA = BLOCKS < MB ? BLOCKS : MB;
+    static_assert(RA > 0 && MB % RA == 0, "");
+    constexpr int SPREAD = BN / 4 < 32 ? BN / 4 - 1 : 31;
+    constexpr int COLS = FORM == GATE ? BN / 2 : BN, PER = COLS / 8, TURNS = 32 * RA * WM * PER / (64 * W), MOST = 16 / E / 2, CH = FORM != DACT ? 1 : TURNS < MOST ? TURNS : MOST;
+    static_assert(TURNS % CH == 0, "");
+    const int width = FORM == GATE ? P.F : P.N;
+    const int c8 = t % PER, n = n0 + 8 * c8;      // (64 W is a multiple of PER)
 #pragma unroll
-    for (int a = 0; a < MB; ++a) {
-        const long long m = m0 + wm + 32 * a + ln;
-        if (m >= P.M) continue;
-        if constexpr (FORM == GATE) {
+    for (int a0 = 0; a0 < MB; a0 += RA) {
+    auto row_of = [&](int turn) {                 // of LDS
+        return (turn * 64 * W + t) / PER;
+    };
+    auto m_of = [&](int row) { return m0 + row / (32 * RA) * (32 * MB) + 32 * a0 + row % (32 * RA); };
+    Eight<T> g8[CH], u8[CH];
+    auto request = [&](int turn) {
+        if constexpr (FORM == DACT)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int f = n0 + wn / 2 + 8 * i + 4 * half;
-                if (f >= P.F) continue;
-                float g[4], u[4], h[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    g[j] = acc[a][0][4 * i + j];
-                    u[j] = acc[a][1][4 * i + j];
-                    h[j] = activation(g[j], P.act) * u[j];      // (of the sums, not of what is kept of them)
-                }
-                store4((T*)P.out + m * P.F + f, h);
-                if (P.out2) {
-                    store4((T*)P.out2 + m * 2 * P.F + f, g);
-                    store4((T*)P.out2 + m * 2 * P.F + P.F + f, u);
+            for (int i = 0; i < CH; ++i) {
+                const long long m = m_of(row_of(turn + i));
+                if (m < P.M && n < width) {
+                    const T* at = (const T*)P.gu + m * 2 * width + n;
+                    g8[i] = *(const Eight<T>*)at;
+                    u8[i] = *(const Eight<T>*)(at + width);
                 }
             }
-        } else {
+    };
+    request(0);
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");      // all waves have read the last step, or the results before
+    {
+        const int ln = lane & 31, half = lane >> 5;
+#pragma unroll
+        for (int a = 0; a < RA; ++a)
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int n = n0 + wn + 32 * b + 8 * i + 4 * half;
-                    if (n >= P.N) continue;
-                    float v[4];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) v[j] = acc[a][b][4 * i + j];
-                    if constexpr (FORM == STORE) store4((T*)P.out + m * P.N + n, v);
-                    if constexpr (FORM == PART) store4((float*)P.out + ((long long)split * P.M + m) * P.N + n, v);
-                    if constexpr (FORM == DACT) {
-                        float g[4], u[4], h[4];
-                        load4((const T*)P.gu + m * 2 * P.N + n, g);
-                        load4((const T*)P.gu + m * 2 * P.N + P.N + n, u);
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            float c, d;
-                            activation(g[j], P.act, c, d);
-                            h[j] = c * u[j];
-                            g[j] = v[j] * u[j] * d;
-                            u[j] = v[j] * c;
-                        }
-                        store4((T*)P.out + m * P.N + n, h);
-                        store4((T*)P.out2 + m * 2 * P.N + n, g);
-                        store4((T*)P.out2 + m * 2 * P.N + P.N + n, u);
-                    }
+                    const f32x16& v = acc[a0 + a][b];
+                    const int row = wave % WM * 32 * RA + 32 * a + ln, piece = (wn + 32 * b + 8 * i + 4 * half) / 4;
+                    *(float4*)(lds + row * BN * 4 + ((piece ^ (ln & SPREAD)) << 4)) = float4{v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]};
                 }
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    auto take = [&](int row, int col, float (&v)[8]) {      // eight results, col a multiple of 8
+        const char* l = lds + row * BN * 4;
+        const float4 x = *(const float4*)(l + (((col / 4) ^ (row & SPREAD)) << 4)), y = *(const float4*)(l + (((col / 4 + 1) ^ (row & SPREAD)) << 4));
+        v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w; v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
+    };
+#pragma unroll
+    for (int turn = 0; turn < TURNS; turn += CH) {
+        float g[CH][8], u[CH][8];
+        if constexpr (FORM == DACT) {
+#pragma unroll
+            for (int i = 0; i < CH; ++i) {
+                g8[i].unpack(g[i]);
+                u8[i].unpack(u[i]);
+            }
+            if (turn + CH < TURNS) request(turn + CH);
         }
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            const int row = row_of(turn + i);
+            const long long m = m_of(row);
+            if (m >= P.M || n >= width) continue;
+            float v[8];
+            if constexpr (FORM == GATE) {
+                take(row, (c8 >> 2) * 64 + (c8 & 3) * 8, g[0]);
+                take(row, (c8 >> 2) * 64 + (c8 & 3) * 8 + 32, u[0]);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = activation<T>(g[0][j], P.act) * u[0][j];      // (of the sums, not of what is kept of them)
+                store_values<T, 8>((T*)P.out + m * width + n, v);
+                if (P.out2) {
+                    store_values<T, 8>((T*)P.out2 + m * 2 * width + n, g[0]);
+                    store_values<T, 8>((T*)P.out2 + m * 2 * width + width + n, u[0]);
+                }
+                continue;
+            }
+            take(row, 8 * c8, v);
+            if constexpr (FORM == STORE) store_values<T, 8>((T*)P.out + m * width + n, v);
+            if constexpr (FORM == PART) store_values<float, 8>((float*)P.out + ((long long)split * P.M + m) * width + n, v);
+            if constexpr (FORM == DACT) {
+                float h[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    float c, d;
+                    activation<T>(g[i][j], P.act, c, d);
+                    h[j] = c * u[i][j];
+                    g[i][j] = v[j] * u[i][j] * d;
+                    u[i][j] = v[j] * c;
+                }
+                store_values<T, 8>((T*)P.out + m * width + n, h);
+                store_values<T, 8>((T*)P.out2 + m * 2 * width + n, g[i]);
+                store_values<T, 8>((T*)P.out2 + m * 2 * width + width + n, u[i]);
+            }
+        }
+    }
     }
 }
 
 long long tiles_of(long long n, int tile) { return (n + tile - 1) / tile; }
 
-template <typename T, bool QA, bool PA, Form FORM>
-int gemm(FfnParams P, hipStream_t s) {
-    constexpr int MB = 2, WM = 2, WN = 2, BM = 32 * MB * WM, BN = 64 * WN, STAGES = 2 * (BM + BN) * 128;
+template <typename T, int MB, int WM, int WN, int KB, int RING, bool QA, bool PA, Form FORM>
+int launch(FfnParams P, hipStream_t s) {
+    constexpr int BM = 32 * MB * WM, BN = 64 * WN, STAGES = RING * (BM + BN) * KB;
     P.mt = (int)tiles_of(P.M, BM);
     P.nt = (int)tiles_of(FORM == GATE ? P.F : P.N, FORM == GATE ? BN / 2 : BN);
-    P.steps = tiles_of(P.K, 128 / sizeof(T));
+    P.steps = tiles_of(P.K, KB / sizeof(T));
     if (P.splits < 1) P.splits = 1;
-    const auto kernel = ffn_gemm_kernel<T, MB, WM, WN, QA, PA, FORM>;
+    const auto kernel = ffn_gemm_kernel<T, MB, WM, WN, KB, RING, QA, PA, FORM>;
     const long long grid = (long long)P.mt * P.nt * P.splits;
     if (grid == 0) return MI3D_OK;
     if (grid >= (1ll << 31)) return MI3D_ERR_UNSUPPORTED;
@@ -310,12 +364,83 @@ int gemm(FfnParams P, hipStream_t s) {
     return check_launch();
 }
 
-// parts of the contraction of a weight gradient, so that its tiles fill the chip
-int wgrad_splits(long long M, long long N, long long K, int e) {
-    const long long tiles = tiles_of(M, 128) * tiles_of(N, 128), steps = tiles_of(K, 128 / e);
-    long long s = 2 * 256 / tiles;
-    if (s > steps / 4) s = steps / 4;
-    return (int)(s < 1 ? 1 : s > 64 ? 64 : s);
+// ---- which kernel, and into how many parts the contraction goes -----------------------------------------------------------
+//
+// The time of a product on tiles is rounds of workgroups (one or two on a compute unit), each of which takes a fixed time (first
+// loads, results) and a time for every 128 bytes of k; less where it has its compute unit for itself.  Microseconds, measured over
+// 300 to 27648 rows, 200 to 4096 channels and F 520 to 8192 (the design doc has the table):
+//   LARGE  256 x 256, 8 waves: 1.36 PFLOP/s on long contractions, where LDS reads per product are fewest, but alone on its unit
+//   MIDDLE 128 x 128: two on a unit, which cover each other's first loads and results; best for short contractions
+//   SMALL  64 x 128: fills the chip with a quarter of the rows
+//   FEW    no LDS (ffn_few.hip): small matrices and few rows
+enum Tile { LARGE, MIDDLE, SMALL, FEW };
+struct TileTimes {
+    int bm, bn, per_cu;
+    double fixed, dact, alone, shared;      // per round, the same for the data gradient's first product; per 128 bytes of k
+};
+constexpr TileTimes TIMES_BF16[3] = {{256, 256, 1, 12.0, 34.0, 1.6, 1.6}, {128, 128, 2, 4.8, 14.0, 0.70, 1.09}, {64, 128, 2, 3.7, 8.6, 0.38, 0.68}};
+constexpr TileTimes TIMES_F32[3] = {{256, 256, 1, 12.0, 34.0, 7.8, 7.8}, {128, 128, 2, 4.8, 14.0, 2.2, 3.7}, {64, 128, 2, 3.7, 8.6, 1.2, 2.1}};
+
+struct Plan {
+    Tile tile;
+    int splits;
+    double us;
+};
+double tiles_us(const TileTimes& t, bool dact, long long tiles, double steps) {
+    const long long cus = cu_count(), slots = t.per_cu * cus, rest = tiles % slots;
+    const double fixed = dact ? t.dact : t.fixed;
+    return (double)(tiles / slots) * (fixed + steps * t.shared) + (rest == 0 ? 0.0 : rest <= cus ? fixed + steps * t.alone : fixed + steps * t.shared);
+}
+// cols: columns of D that tiles cover (GATE: of both halves).  most_parts 1: the contraction is not split
+Plan plan(Form form, int e, long long M, long long cols, long long K, int most_parts) {
+    Plan best{MIDDLE, 1, 1e30};
+    const double steps = (double)tiles_of(K * e, 128);
+    for (int i = e == 2 ? 0 : 1; i < 3; ++i) {      // (fp32: LARGE has nothing to save, the matrix instructions take eight times longer)
+        const TileTimes& t = (e == 2 ? TIMES_BF16 : TIMES_F32)[i];
+        const long long tiles = tiles_of(M, t.bm) * tiles_of(cols, t.bn);
+        for (int s = 1; s <= most_parts && (s == 1 || s * 4 <= steps); s += s < 8 ? 1 : s / 4) {
+            const double us = tiles_us(t, form == DACT, tiles * s, steps / s) + (s > 1 ? 3.0 + (s + 1.0) * 4.0 * M * cols / 6e6 : 0.0);
+            if (us < best.us) best = Plan{(Tile)i, s, us};
+        }
+    }
+    if (form == GATE || form == STORE) {
+        const double us = few_rows_us(e == 2, form == GATE, M, K, form == GATE ? cols / 2 : cols);
+        if (us < best.us) best = Plan{FEW, 1, us};
+    }
+    return best;
+}
+constexpr int MOST_PARTS = 64;
+
+template <typename T, bool QA, bool PA, Form FORM>
+int gemm(const FfnParams& P, Tile tile, hipStream_t s) {
+    if constexpr (sizeof(T) == 2)
+        if (tile == LARGE) return launch<T, 4, 2, 4, 64, 4, QA, PA, FORM>(P, s);
+    if (tile == MIDDLE) return launch<T, 2, 2, 2, 128, 2, QA, PA, FORM>(P, s);
+    return launch<T, 1, 2, 2, 128, 3, QA, PA, FORM>(P, s);
+}
+
+// dx = sum of the parts, rounded.  A workgroup serves 256 values: thread (slice, eight values) adds parts slice, slice + 8, ..., and the
+// eight sums are added in order.
+template <typename T>
+__global__ void __launch_bounds__(256) ffn_add_parts_kernel(const float* __restrict__ part, T* __restrict__ out, long long n, int parts) {
+    __shared__ float red[8][256];
+    const int t = threadIdx.x, slice = t >> 5;
+    const long long at = (long long)blockIdx.x * 256 + 8 * (t & 31);
+    float v[8] = {}, o[8];
+    if (at < n)
+        for (int p = slice; p < parts; p += 8) {
+            load_values<float, 8>(part + p * n + at, o);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] += o[j];
+        }
+    store_values<float, 8>(&red[slice][8 * (t & 31)], v);
+    __syncthreads();
+    const long long i = (long long)blockIdx.x * 256 + t;
+    if (i >= n) return;
+    o[0] = red[0][t];
+    for (int p = 1; p < 8 && p < parts; ++p) o[0] += red[p][t];
+    const float r[1] = {o[0]};
+    store_values<T, 1>(out + i, r);
 }
 
 struct Desc {
@@ -332,48 +457,63 @@ int make(const mi3d_ffn_desc* d, Desc* o) {
     return MI3D_OK;
 }
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
+Plan dx_plan(const Desc& d) { return plan(PART, d.e, d.rows, d.C, 2 * d.F, MOST_PARTS); }
+Plan outer_plan(long long rows, int M, int N, int e) { return plan(PART, e, M, N, rows, MOST_PARTS); }
+size_t parts_bytes(int splits, long long M, long long N) { return splits > 1 ? (size_t)splits * M * N * 4 : 0; }
+bool usable(const void* p) { return p && aligned16(p); }
+
 size_t workspace(const Desc& d, int pass) {
     if (pass == MI3D_PASS_FWD) return round256((size_t)d.rows * d.F * d.e);      // h
+    if (pass == MI3D_PASS_DGRAD) return d.rows ? parts_bytes(dx_plan(d).splits, d.rows, d.C) : 0;
     if (pass != MI3D_PASS_WGRAD) return 0;
-    const int s1 = wgrad_splits(2 * d.F, d.C, d.rows, d.e), s2 = wgrad_splits(d.O, d.F, d.rows, d.e);
-    const size_t n1 = s1 > 1 ? (size_t)s1 * 2 * d.F * d.C * 4 : 0, n2 = s2 > 1 ? (size_t)s2 * d.O * d.F * 4 : 0;
+    const size_t n1 = parts_bytes(outer_plan(d.rows, 2 * d.F, d.C, d.e).splits, 2 * d.F, d.C), n2 = parts_bytes(outer_plan(d.rows, d.O, d.F, d.e).splits, d.O, d.F);
     return n1 > n2 ? n1 : n2;
 }
-bool usable(const void* p) { return p && aligned16(p); }
 
 template <typename T>
 int gate(const Desc& d, const void* x, const void* w1, void* h, void* gu, hipStream_t s) {
+    const Plan p = plan(GATE, d.e, d.rows, 2 * d.F, d.C, 1);
+    if (p.tile == FEW) return few_rows_product(sizeof(T) == 2, true, x, w1, d.rows, d.C, d.F, d.act, h, gu, s);
     FfnParams P{};
     P.q = x; P.p = w1; P.M = d.rows; P.K = d.C; P.N = d.F; P.qp = d.C; P.pp = d.C; P.F = d.F; P.act = d.act;
     P.out = h; P.out2 = gu;
-    return gemm<T, false, false, GATE>(P, s);
+    return gemm<T, false, false, GATE>(P, p.tile, s);
 }
 template <typename T>
 int project(const Desc& d, const void* h, const void* w2, void* y, hipStream_t s) {
+    const Plan p = plan(STORE, d.e, d.rows, d.O, d.F, 1);
+    if (p.tile == FEW) return few_rows_product(sizeof(T) == 2, false, h, w2, d.rows, d.F, d.O, 0, y, nullptr, s);
     FfnParams P{};
     P.q = h; P.p = w2; P.M = d.rows; P.K = d.F; P.N = d.O; P.qp = d.F; P.pp = d.F; P.out = y;
-    return gemm<T, false, false, STORE>(P, s);
+    return gemm<T, false, false, STORE>(P, p.tile, s);
 }
 template <typename T>
-int dgrad(const Desc& d, const void* dy, const void* w1, const void* w2, const void* gu, void* dgu, void* h, void* dx, hipStream_t s) {
+int dgrad(const Desc& d, const void* dy, const void* w1, const void* w2, const void* gu, void* dgu, void* h, void* dx, void* ws, hipStream_t s) {
     FfnParams P{};
     P.q = dy; P.p = w2; P.M = d.rows; P.K = d.O; P.N = d.F; P.qp = d.O; P.pp = d.F; P.act = d.act;
     P.out = h; P.out2 = dgu; P.gu = gu;
-    const int st = gemm<T, false, true, DACT>(P, s);
+    int st = gemm<T, false, true, DACT>(P, plan(DACT, d.e, d.rows, d.F, d.O, 1).tile, s);
     if (st) return st;
+    const Plan p = dx_plan(d);
     FfnParams R{};
-    R.q = dgu; R.p = w1; R.M = d.rows; R.K = 2 * d.F; R.N = d.C; R.qp = 2 * d.F; R.pp = d.C; R.out = dx;
-    return gemm<T, false, true, STORE>(R, s);
+    R.q = dgu; R.p = w1; R.M = d.rows; R.K = 2 * d.F; R.N = d.C; R.qp = 2 * d.F; R.pp = d.C; R.splits = p.splits;
+    R.out = p.splits > 1 ? ws : dx;
+    if (p.splits == 1) return gemm<T, false, true, STORE>(R, p.tile, s);
+    st = gemm<T, false, true, PART>(R, p.tile, s);
+    if (st) return st;
+    const long long n = d.rows * d.C;
+    ffn_add_parts_kernel<T><<<(unsigned)tiles_of(n, 256), 256, 0, s>>>((const float*)ws, (T*)dx, n, p.splits);
+    return check_launch();
 }
 // out[m][n] = sum over rows of a[row][m] b[row][n]
 template <typename T>
 int outer(const void* a, const void* b, long long rows, int M, int N, float* out, void* ws, hipStream_t s) {
+    const Plan p = outer_plan(rows, M, N, sizeof(T));
     FfnParams P{};
-    P.q = a; P.p = b; P.M = M; P.K = rows; P.N = N; P.qp = M; P.pp = N;
-    P.splits = wgrad_splits(M, N, rows, sizeof(T));
-    P.out = P.splits > 1 ? ws : out;
-    const int st = gemm<T, true, true, PART>(P, s);
-    return st || P.splits == 1 ? st : reduce_partials((const float*)ws, out, (long long)M * N, P.splits, s);
+    P.q = a; P.p = b; P.M = M; P.K = rows; P.N = N; P.qp = M; P.pp = N; P.splits = p.splits;
+    P.out = p.splits > 1 ? ws : out;
+    const int st = gemm<T, true, true, PART>(P, p.tile, s);
+    return st || p.splits == 1 ? st : reduce_partials((const float*)ws, out, (long long)M * N, p.splits, s);
 }
 
 }  // namespace
@@ -423,7 +563,7 @@ int mi3d_ffn_dgrad(const mi3d_ffn_desc* desc, const void* dy, const void* w1, co
     if (!dy || !gu || !dgu || !h || !dx) return MI3D_ERR_INVALID_ARG;
     const size_t need = workspace(d, MI3D_PASS_DGRAD);
     if (need && (!ws || ws_bytes < need)) return MI3D_ERR_WORKSPACE;
-    return d.e == 2 ? dgrad<uint16_t>(d, dy, w1, w2, gu, dgu, h, dx, (hipStream_t)stream) : dgrad<float>(d, dy, w1, w2, gu, dgu, h, dx, (hipStream_t)stream);
+    return d.e == 2 ? dgrad<uint16_t>(d, dy, w1, w2, gu, dgu, h, dx, ws, (hipStream_t)stream) : dgrad<float>(d, dy, w1, w2, gu, dgu, h, dx, ws, (hipStream_t)stream);
 }
 
 int mi3d_ffn_wgrad(const mi3d_ffn_desc* desc, const void* x, const void* dgu, const void* h, const void* dy, float* dw1, float* dw2,
