@@ -8,9 +8,9 @@ namespace mi3d {
 // act(g) and act'(g); silu: g s(g) with the logistic s, gelu: g Phi(g) with the normal distribution's Phi.  bf16: the hardware's
 // exponential and reciprocal, and Phi from the rational approximation 7.1.26 of Abramowitz and Stegun's Handbook (error
 // of erf below 1.5e-7), whose exponential is that of the derivative as well; fp32: the library's functions.
-template <typename T>
-__device__ __forceinline__ void activation(float g, int act, float& a, float& d) {
-    if (act == MI3D_ACT_SILU) {
+template <typename T, int ACT>
+__device__ __forceinline__ void activation(float g, float& a, float& d) {
+    if constexpr (ACT == MI3D_ACT_SILU) {
         const float s = sizeof(T) == 2 ? __builtin_amdgcn_rcpf(1.f + __expf(-g)) : 1.f / (1.f + expf(-g));
         a = g * s;
         d = fmaf(a, 1.f - s, s);
@@ -28,13 +28,12 @@ __device__ __forceinline__ void activation(float g, int act, float& a, float& d)
         d = fmaf(g * 0.39894228f, e, c);
     }
 }
-template <typename T>
-__device__ __forceinline__ float activation(float g, int act) {
+template <typename T, int ACT>
+__device__ __forceinline__ float activation(float g) {
     float a, d;
-    activation<T>(g, act, a, d);
+    activation<T, ACT>(g, a, d);
     return a;
 }
-
 
 // The forward products of few rows, or of small matrices.  gated: w holds 2 N rows, out = act(g) * u (and [g | u] where gu is not
 // null); otherwise N rows and out = x w^T.  K and N are multiples of 8.  few_rows_us: what its model expects it to take (very long:

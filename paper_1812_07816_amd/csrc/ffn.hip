@@ -28,11 +28,12 @@ struct FfnParams {
     const void *q, *p;
     long long M, K;
     int N, qp, pp;             // columns of D; elements from one row of Q's and P's memory to the next
-    int F, act;
+    int F;
     void *out, *out2;          // STORE, PART: D.  GATE: h, [g | u] or null.  DACT: h, [dg | du]
     const void* gu;            // DACT
-    int mt, nt, splits;
-    long long steps;
+    int splits, per, extra;    // parts of the contraction; steps of a part, one more of the first `extra`
+    Div tiles, band, last;     // of a part, of four tiles of rows (`last`: of rows in the last such band)
+    int mt, nt;
 };
 
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const char* p, long long bytes) {
@@ -40,14 +41,15 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const char* p, long lon
 }
 
 // eight values as they lie in memory
-template <typename T> struct Eight;
-template <> struct Eight<uint16_t> {
-    uint4 v;
-    __device__ __forceinline__ void unpack(float (&f)[8]) const { load_values<uint16_t, 8>((const uint16_t*)&v, f); }
-};
-template <> struct Eight<float> {
-    float4 v[2];
-    __device__ __forceinline__ void unpack(float (&f)[8]) const { load_values<float, 8>((const float*)v, f); }
+typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t u32x4;
+template <typename T>
+struct Eight {
+    u32x4 v[sizeof(T) / 2];
+    __device__ __forceinline__ void load_streamed(const T* p) {
+#pragma unroll
+        for (int i = 0; i < (int)(sizeof(T) / 2); ++i) v[i] = __builtin_nontemporal_load((const u32x4*)p + i);
+    }
+    __device__ __forceinline__ void unpack(float (&f)[8]) const { load_values<T, 8>((const T*)v, f); }
 };
 
 // One operand's share of a step in LDS: R rows of KB bytes of k (ACROSS false), or KB / sizeof(T) rows of k of R values.  16-byte
@@ -94,8 +96,8 @@ struct Operand {
 
 // A workgroup of WM x WN waves owns 32 MB WM rows x 64 WN columns of D (GATE: columns of g and of u, half each); a wave MB x 2 blocks of
 // 32 x 32.  A step is KB bytes of k; RING steps have a place in LDS, RING - 1 are under way while one is computed.
-template <typename T, int MB, int WM, int WN, int KB, int RING, bool QA, bool PA, Form FORM>
-__global__ void __launch_bounds__(64 * WM * WN, 2) ffn_gemm_kernel(const FfnParams P) {
+template <typename T, int MB, int WM, int WN, int KB, int RING, bool QA, bool PA, Form FORM, int ACT>
+__device__ __forceinline__ void ffn_tile(const FfnParams& P, const int block) {
     constexpr int W = WM * WN, BM = 32 * MB * WM, BN = 64 * WN, E = sizeof(T), KS = KB / E;
     constexpr int NQ = BM * KB / 1024 / W, NP = BN * KB / 1024 / W, Q_BYTES = BM * KB, STAGE = (BM + BN) * KB;
     constexpr int ROWS = 1024 / KB;      // (k along) rows of a wave's load
@@ -105,17 +107,17 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) ffn_gemm_kernel(const FfnPara
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
 
     // block -> (part, tile); the blocks of an XCD (every eighth) get neighbouring tiles, four tiles of rows by all of columns at a time
-    const int tiles = P.mt * P.nt;
     int id;
     {
-        const int n = tiles * P.splits, l = blockIdx.x, x = l & 7, q = l >> 3;
+        const int n = (int)P.tiles.d * P.splits, l = block, x = l & 7, q = l >> 3;
         id = x * (n >> 3) + ((n & 7) < x ? (n & 7) : x) + q;
     }
-    const int split = id / tiles;
-    id -= split * tiles;
-    const int band = id / (4 * P.nt), in = id - band * 4 * P.nt, high = P.mt - 4 * band < 4 ? P.mt - 4 * band : 4;
-    const int mt = 4 * band + in % high, nt = in / high;
-    const long long s0 = P.steps * split / P.splits, s1 = P.steps * (split + 1) / P.splits;
+    const int split = divide(id, P.tiles);
+    id -= split * (int)P.tiles.d;
+    const int band = divide(id, P.band), in = id - band * (int)P.band.d;
+    const bool whole = 4 * band + 4 <= P.mt;
+    const int nt = whole ? in >> 2 : divide(in, P.last), mt = 4 * band + (whole ? in & 3 : in - nt * (int)P.last.d);
+    const int s0 = split * P.per + (split < P.extra ? split : P.extra), s1 = s0 + P.per + (split < P.extra ? 1 : 0);
 
     const long long m0 = (long long)mt * BM, kbytes = P.K * E;
     const int n0 = nt * (FORM == GATE ? BN / 2 : BN);
@@ -149,14 +151,14 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) ffn_gemm_kernel(const FfnPara
     unsigned slot_in = 0, to = 0;
     bool inside = false;                                 // (k along) this lane's piece lies before the end of k
     __amdgpu_buffer_rsrc_t rq = buffer(q, 0), rp = rq, ru = rq;
-    auto begin = [&](long long s) {
+    auto begin = [&](int s) {
         to = lds_wave + slot_in * STAGE;
         slot_in = slot_in + 1 == RING ? 0 : slot_in + 1;
-        const long long k = s * KB, none = s < s1 ? 0 : 1ll << 62;
+        const long long k = (long long)s * KB, none = s < s1 ? 0 : 1ll << 62;
         inside = k + kq < kbytes;
-        const long long aq = QA ? s * KS * qrow + m0 * E : m0 * qrow + k;
+        const long long aq = QA ? (long long)s * KS * qrow + m0 * E : m0 * qrow + k;
         rq = buffer(q + aq, (QA ? P.K : P.M) * qrow - aq - none);
-        const long long ap = PA ? s * KS * prow + (long long)n0 * E : n0 * prow + k;
+        const long long ap = PA ? (long long)s * KS * prow + (long long)n0 * E : n0 * prow + k;
         const long long all = PA ? P.K * prow : (FORM == GATE ? P.F : P.N) * prow;
         rp = buffer(p + ap, all - ap - none);
         if (FORM == GATE) ru = buffer(p + ap + all, all - ap - none);
@@ -206,7 +208,7 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) ffn_gemm_kernel(const FfnPara
     }
     const char* l = lds;
     unsigned slot = 0;
-    for (long long s = s0; s < s1; ++s) {
+    for (int s = s0; s < s1; ++s) {
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk) {
             if (kk == KK - 1) {
@@ -240,6 +242,8 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) ffn_gemm_kernel(const FfnPara
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // (the loads behind the last step)
 
+    // (GATE, DACT: what comes and goes here is several times what the operands are, which stay in L2 if it is streamed past them: the two
+    // products of 16384 x 1024 x 4096's data gradient 238 + 233 -> 229 + 214 us.)
     // The results go through LDS (a lane holds four columns of one row; 16-byte pieces permuted by the row) so that each row's are
     // read and written in whole lines, eight values a thread, RA of the MB blocks of rows at a time.  The data gradient's g and u
     // are requested before.
@@ -264,8 +268,8 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) ffn_gemm_kernel(const FfnPara
                 const long long m = m_of(row_of(turn + i));
                 if (m < P.M && n < width) {
                     const T* at = (const T*)P.gu + m * 2 * width + n;
-                    g8[i] = *(const Eight<T>*)at;
-                    u8[i] = *(const Eight<T>*)(at + width);
+                    g8[i].load_streamed(at);
+                    u8[i].load_streamed(at + width);
                 }
             }
     };
@@ -311,11 +315,11 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) ffn_gemm_kernel(const FfnPara
                 take(row, (c8 >> 2) * 64 + (c8 & 3) * 8, g[0]);
                 take(row, (c8 >> 2) * 64 + (c8 & 3) * 8 + 32, u[0]);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = activation<T>(g[0][j], P.act) * u[0][j];      // (of the sums, not of what is kept of them)
-                store_values<T, 8>((T*)P.out + m * width + n, v);
+                for (int j = 0; j < 8; ++j) v[j] = activation<T, ACT>(g[0][j]) * u[0][j];      // (of the sums, not of what is kept of them)
+                store_streamed<T>((T*)P.out + m * width + n, v);
                 if (P.out2) {
-                    store_values<T, 8>((T*)P.out2 + m * 2 * width + n, g[0]);
-                    store_values<T, 8>((T*)P.out2 + m * 2 * width + width + n, u[0]);
+                    store_streamed<T>((T*)P.out2 + m * 2 * width + n, g[0]);
+                    store_streamed<T>((T*)P.out2 + m * 2 * width + width + n, u[0]);
                 }
                 continue;
             }
@@ -327,40 +331,88 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) ffn_gemm_kernel(const FfnPara
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     float c, d;
-                    activation<T>(g[i][j], P.act, c, d);
+                    activation<T, ACT>(g[i][j], c, d);
                     h[j] = c * u[i][j];
                     g[i][j] = v[j] * u[i][j] * d;
                     u[i][j] = v[j] * c;
                 }
-                store_values<T, 8>((T*)P.out + m * width + n, h);
-                store_values<T, 8>((T*)P.out2 + m * 2 * width + n, g[i]);
-                store_values<T, 8>((T*)P.out2 + m * 2 * width + width + n, u[i]);
+                store_streamed<T>((T*)P.out + m * width + n, h);
+                store_streamed<T>((T*)P.out2 + m * 2 * width + n, g[i]);
+                store_streamed<T>((T*)P.out2 + m * 2 * width + width + n, u[i]);
             }
         }
     }
     }
 }
 
+template <typename T, int MB, int WM, int WN, int KB, int RING, bool QA, bool PA, Form FORM, int ACT>
+__global__ void __launch_bounds__(64 * WM * WN, 2) ffn_gemm_kernel(const FfnParams P) {
+    ffn_tile<T, MB, WM, WN, KB, RING, QA, PA, FORM, ACT>(P, blockIdx.x);
+}
+// Two products in one launch, the second one's workgroups from block `first` on (a multiple of 8)
+struct FfnPair {
+    FfnParams a, b;
+    int first;
+};
+template <typename T, int MB, int WM, int WN, int KB, int RING>
+__global__ void __launch_bounds__(64 * WM * WN, 2) ffn_outer_pair_kernel(const FfnPair P) {
+    const bool second = (int)blockIdx.x >= P.first;
+    const FfnParams& R = second ? P.b : P.a;
+    const int block = blockIdx.x - (second ? P.first : 0);
+    if (block >= (int)R.tiles.d * R.splits) return;      // (fills up to `first`)
+    ffn_tile<T, MB, WM, WN, KB, RING, true, true, PART, 0>(R, block);
+}
+
 long long tiles_of(long long n, int tile) { return (n + tile - 1) / tile; }
 
-template <typename T, int MB, int WM, int WN, int KB, int RING, bool QA, bool PA, Form FORM>
+// what the kernel needs to find its tile; false: too many
+bool number_tiles(FfnParams* P, int bm, int cols, int bn, int ks) {
+    P->mt = (int)tiles_of(P->M, bm);
+    P->nt = (int)tiles_of(cols, bn);
+    const long long tiles = (long long)P->mt * P->nt, steps = tiles_of(P->K, ks);
+    if (P->splits < 1) P->splits = 1;
+    if (tiles * P->splits >= (1ll << 30) || steps >= (1ll << 31)) return false;
+    P->per = (int)(steps / P->splits);
+    P->extra = (int)(steps % P->splits);
+    P->tiles = make_div((uint32_t)tiles);
+    P->band = make_div(4u * P->nt);
+    P->last = make_div(P->mt % 4 ? P->mt % 4 : 4);
+    return true;
+}
+template <class Kernel>
+int allow_lds(Kernel kernel, int bytes) {
+    const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != hipSuccess) note_hip_error(e);
+    return e == hipSuccess ? MI3D_OK : MI3D_ERR_HIP;
+}
+
+template <typename T, int MB, int WM, int WN, int KB, int RING, bool QA, bool PA, Form FORM, int ACT>
 int launch(FfnParams P, hipStream_t s) {
-    constexpr int BM = 32 * MB * WM, BN = 64 * WN, STAGES = RING * (BM + BN) * KB;
-    P.mt = (int)tiles_of(P.M, BM);
-    P.nt = (int)tiles_of(FORM == GATE ? P.F : P.N, FORM == GATE ? BN / 2 : BN);
-    P.steps = tiles_of(P.K, KB / sizeof(T));
-    if (P.splits < 1) P.splits = 1;
-    const auto kernel = ffn_gemm_kernel<T, MB, WM, WN, KB, RING, QA, PA, FORM>;
-    const long long grid = (long long)P.mt * P.nt * P.splits;
-    if (grid == 0) return MI3D_OK;
-    if (grid >= (1ll << 31)) return MI3D_ERR_UNSUPPORTED;
+    constexpr int BM = 32 * MB * WM, BN = 64 * WN, LDS = RING * (BM + BN) * KB;
+    if (!number_tiles(&P, BM, FORM == GATE ? P.F : P.N, FORM == GATE ? BN / 2 : BN, KB / sizeof(T))) return MI3D_ERR_UNSUPPORTED;
+    const auto kernel = ffn_gemm_kernel<T, MB, WM, WN, KB, RING, QA, PA, FORM, ACT>;
     static std::atomic<bool> attr_set{false};   // set once per process; a second thread racing here repeats an idempotent call
     if (!attr_set) {
-        const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, STAGES);
-        if (e != hipSuccess) { note_hip_error(e); return MI3D_ERR_HIP; }
+        const int st = allow_lds(kernel, LDS);
+        if (st) return st;
         attr_set = true;
     }
-    kernel<<<(unsigned)grid, 64 * WM * WN, STAGES, s>>>(P);
+    kernel<<<P.tiles.d * P.splits, 64 * WM * WN, LDS, s>>>(P);
+    return check_launch();
+}
+template <typename T, int MB, int WM, int WN, int KB, int RING>
+int launch_pair(FfnPair P, hipStream_t s) {
+    constexpr int BM = 32 * MB * WM, BN = 64 * WN, LDS = RING * (BM + BN) * KB;
+    if (!number_tiles(&P.a, BM, P.a.N, BN, KB / sizeof(T)) || !number_tiles(&P.b, BM, P.b.N, BN, KB / sizeof(T))) return MI3D_ERR_UNSUPPORTED;
+    P.first = (int)(P.a.tiles.d * P.a.splits + 7) / 8 * 8;
+    const auto kernel = ffn_outer_pair_kernel<T, MB, WM, WN, KB, RING>;
+    static std::atomic<bool> attr_set{false};
+    if (!attr_set) {
+        const int st = allow_lds(kernel, LDS);
+        if (st) return st;
+        attr_set = true;
+    }
+    kernel<<<P.first + P.b.tiles.d * P.b.splits, 64 * WM * WN, LDS, s>>>(P);
     return check_launch();
 }
 
@@ -391,15 +443,18 @@ double tiles_us(const TileTimes& t, bool dact, long long tiles, double steps) {
     const double fixed = dact ? t.dact : t.fixed;
     return (double)(tiles / slots) * (fixed + steps * t.shared) + (rest == 0 ? 0.0 : rest <= cus ? fixed + steps * t.alone : fixed + steps * t.shared);
 }
-// cols: columns of D that tiles cover (GATE: of both halves).  most_parts 1: the contraction is not split
-Plan plan(Form form, int e, long long M, long long cols, long long K, int most_parts) {
+// time of adding the parts of n sums
+double add_us(int splits, double n) { return splits > 1 ? 3.0 + (splits + 1.0) * 4.0 * n / 5e6 : 0.0; }
+// cols: columns of D that tiles cover (GATE: of both halves).  most_parts 1: the contraction is not split.  M2 x cols2: a second product
+// with the same contraction in the same launch
+Plan plan(Form form, int e, long long M, long long cols, long long K, int most_parts, long long M2 = 0, long long cols2 = 0) {
     Plan best{MIDDLE, 1, 1e30};
     const double steps = (double)tiles_of(K * e, 128);
     for (int i = e == 2 ? 0 : 1; i < 3; ++i) {      // (fp32: LARGE has nothing to save, the matrix instructions take eight times longer)
         const TileTimes& t = (e == 2 ? TIMES_BF16 : TIMES_F32)[i];
-        const long long tiles = tiles_of(M, t.bm) * tiles_of(cols, t.bn);
+        const long long tiles = tiles_of(M, t.bm) * tiles_of(cols, t.bn) + tiles_of(M2, t.bm) * tiles_of(cols2, t.bn);
         for (int s = 1; s <= most_parts && (s == 1 || s * 4 <= steps); s += s < 8 ? 1 : s / 4) {
-            const double us = tiles_us(t, form == DACT, tiles * s, steps / s) + (s > 1 ? 3.0 + (s + 1.0) * 4.0 * M * cols / 6e6 : 0.0);
+            const double us = tiles_us(t, form == DACT, tiles * s, steps / s) + add_us(s, (double)M * cols + (double)M2 * cols2);
             if (us < best.us) best = Plan{(Tile)i, s, us};
         }
     }
@@ -411,36 +466,65 @@ Plan plan(Form form, int e, long long M, long long cols, long long K, int most_p
 }
 constexpr int MOST_PARTS = 64;
 
-template <typename T, bool QA, bool PA, Form FORM>
-int gemm(const FfnParams& P, Tile tile, hipStream_t s) {
+template <typename T, bool QA, bool PA, Form FORM, int ACT>
+int on_tiles(const FfnParams& P, Tile tile, hipStream_t s) {
     if constexpr (sizeof(T) == 2)
-        if (tile == LARGE) return launch<T, 4, 2, 4, 64, 4, QA, PA, FORM>(P, s);
-    if (tile == MIDDLE) return launch<T, 2, 2, 2, 128, 2, QA, PA, FORM>(P, s);
-    return launch<T, 1, 2, 2, 128, 3, QA, PA, FORM>(P, s);
+        if (tile == LARGE) return launch<T, 4, 2, 4, 64, 4, QA, PA, FORM, ACT>(P, s);
+    if (tile == MIDDLE) return launch<T, 2, 2, 2, 128, 2, QA, PA, FORM, ACT>(P, s);
+    return launch<T, 1, 2, 2, 128, 3, QA, PA, FORM, ACT>(P, s);
+}
+template <typename T, bool QA, bool PA, Form FORM>
+int gemm(const FfnParams& P, Tile tile, hipStream_t s, int act = MI3D_ACT_SILU) {
+    if constexpr (FORM == GATE || FORM == DACT)
+        if (act == MI3D_ACT_GELU) return on_tiles<T, QA, PA, FORM, MI3D_ACT_GELU>(P, tile, s);
+    return on_tiles<T, QA, PA, FORM, MI3D_ACT_SILU>(P, tile, s);
 }
 
-// dx = sum of the parts, rounded.  A workgroup serves 256 values: thread (slice, eight values) adds parts slice, slice + 8, ..., and the
-// eight sums are added in order.
+// Sums of the parts of a contraction, rounded to the result's type; of two results one behind the other.  A workgroup has 256 / S groups
+// of eight values: thread (slice, group) adds parts slice, slice + S, ..., and the S sums are added in order.
 template <typename T>
-__global__ void __launch_bounds__(256) ffn_add_parts_kernel(const float* __restrict__ part, T* __restrict__ out, long long n, int parts) {
-    __shared__ float red[8][256];
-    const int t = threadIdx.x, slice = t >> 5;
-    const long long at = (long long)blockIdx.x * 256 + 8 * (t & 31);
+struct Parts {
+    const float* part;      // [parts][n]
+    T* out;
+    long long n;
+    int blocks;
+};
+template <typename T>
+__global__ void __launch_bounds__(256) ffn_add_parts_kernel(const Parts<T> a, const Parts<T> b, int parts, int S) {
+    __shared__ float red[256 * 8];
+    const bool second = (int)blockIdx.x >= a.blocks;
+    const Parts<T>& R = second ? b : a;
+    const int t = threadIdx.x, groups = 256 / S, slice = t / groups, g = t % groups;
+    const long long at = ((long long)blockIdx.x - (second ? a.blocks : 0)) * groups * 8;
     float v[8] = {}, o[8];
-    if (at < n)
-        for (int p = slice; p < parts; p += 8) {
-            load_values<float, 8>(part + p * n + at, o);
+    if (at + 8 * g < R.n)
+        for (int p = slice; p < parts; p += S) {
+            load_values<float, 8>(R.part + p * R.n + at + 8 * g, o);
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] += o[j];
         }
-    store_values<float, 8>(&red[slice][8 * (t & 31)], v);
+    if (S == 1) {
+        if (at + 8 * g < R.n) store_values<T, 8>(R.out + at + 8 * g, v);
+        return;
+    }
+    store_values<float, 8>(red + t * 8, v);
     __syncthreads();
-    const long long i = (long long)blockIdx.x * 256 + t;
-    if (i >= n) return;
-    o[0] = red[0][t];
-    for (int p = 1; p < 8 && p < parts; ++p) o[0] += red[p][t];
-    const float r[1] = {o[0]};
-    store_values<T, 1>(out + i, r);
+    for (int i = t; i < groups * 8; i += 256) {
+        if (at + i >= R.n) break;
+        o[0] = red[i];
+        for (int p = 1; p < S; ++p) o[0] += red[p * groups * 8 + i];
+        const float r[1] = {o[0]};
+        store_values<T, 1>(R.out + at + i, r);
+    }
+}
+template <typename T>
+int add_parts(const float* part, T* out, long long n, const float* part2, T* out2, long long n2, int parts, hipStream_t s) {
+    int S = 1;
+    while (S < 8 && 2 * S <= parts) S *= 2;
+    const int values = 256 / S * 8;
+    const Parts<T> a = {part, out, n, (int)tiles_of(n, values)}, b = {part2, out2, n2, (int)tiles_of(n2, values)};
+    ffn_add_parts_kernel<T><<<(unsigned)(a.blocks + b.blocks), 256, 0, s>>>(a, b, parts, S);
+    return check_launch();
 }
 
 struct Desc {
@@ -458,7 +542,18 @@ int make(const mi3d_ffn_desc* d, Desc* o) {
 }
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 Plan dx_plan(const Desc& d) { return plan(PART, d.e, d.rows, d.C, 2 * d.F, MOST_PARTS); }
-Plan outer_plan(long long rows, int M, int N, int e) { return plan(PART, e, M, N, rows, MOST_PARTS); }
+// Both weight gradients in one launch, or one after the other with parts of their own (16384 x 1024 x 4096: 427 us together, 368 apart;
+// 27000 x 256 x 1024: 68 and 76)
+struct WgradPlan {
+    bool pair;
+    Plan first, second;
+};
+WgradPlan wgrad_plan(const Desc& d) {
+    const Plan both = plan(PART, d.e, 2 * d.F, d.C, d.rows, MOST_PARTS, d.O, d.F);
+    const Plan first = plan(PART, d.e, 2 * d.F, d.C, d.rows, MOST_PARTS), second = plan(PART, d.e, d.O, d.F, d.rows, MOST_PARTS);
+    if (both.us <= first.us + second.us) return WgradPlan{true, both, both};
+    return WgradPlan{false, first, second};
+}
 size_t parts_bytes(int splits, long long M, long long N) { return splits > 1 ? (size_t)splits * M * N * 4 : 0; }
 bool usable(const void* p) { return p && aligned16(p); }
 
@@ -466,8 +561,9 @@ size_t workspace(const Desc& d, int pass) {
     if (pass == MI3D_PASS_FWD) return round256((size_t)d.rows * d.F * d.e);      // h
     if (pass == MI3D_PASS_DGRAD) return d.rows ? parts_bytes(dx_plan(d).splits, d.rows, d.C) : 0;
     if (pass != MI3D_PASS_WGRAD) return 0;
-    const size_t n1 = parts_bytes(outer_plan(d.rows, 2 * d.F, d.C, d.e).splits, 2 * d.F, d.C), n2 = parts_bytes(outer_plan(d.rows, d.O, d.F, d.e).splits, d.O, d.F);
-    return n1 > n2 ? n1 : n2;
+    const WgradPlan p = wgrad_plan(d);
+    const size_t n1 = parts_bytes(p.first.splits, 2 * d.F, d.C), n2 = parts_bytes(p.second.splits, d.O, d.F);
+    return p.pair ? n1 + n2 : n1 > n2 ? n1 : n2;
 }
 
 template <typename T>
@@ -475,9 +571,9 @@ int gate(const Desc& d, const void* x, const void* w1, void* h, void* gu, hipStr
     const Plan p = plan(GATE, d.e, d.rows, 2 * d.F, d.C, 1);
     if (p.tile == FEW) return few_rows_product(sizeof(T) == 2, true, x, w1, d.rows, d.C, d.F, d.act, h, gu, s);
     FfnParams P{};
-    P.q = x; P.p = w1; P.M = d.rows; P.K = d.C; P.N = d.F; P.qp = d.C; P.pp = d.C; P.F = d.F; P.act = d.act;
+    P.q = x; P.p = w1; P.M = d.rows; P.K = d.C; P.N = d.F; P.qp = d.C; P.pp = d.C; P.F = d.F;
     P.out = h; P.out2 = gu;
-    return gemm<T, false, false, GATE>(P, p.tile, s);
+    return gemm<T, false, false, GATE>(P, p.tile, s, d.act);
 }
 template <typename T>
 int project(const Desc& d, const void* h, const void* w2, void* y, hipStream_t s) {
@@ -490,9 +586,9 @@ int project(const Desc& d, const void* h, const void* w2, void* y, hipStream_t s
 template <typename T>
 int dgrad(const Desc& d, const void* dy, const void* w1, const void* w2, const void* gu, void* dgu, void* h, void* dx, void* ws, hipStream_t s) {
     FfnParams P{};
-    P.q = dy; P.p = w2; P.M = d.rows; P.K = d.O; P.N = d.F; P.qp = d.O; P.pp = d.F; P.act = d.act;
+    P.q = dy; P.p = w2; P.M = d.rows; P.K = d.O; P.N = d.F; P.qp = d.O; P.pp = d.F;
     P.out = h; P.out2 = dgu; P.gu = gu;
-    int st = gemm<T, false, true, DACT>(P, plan(DACT, d.e, d.rows, d.F, d.O, 1).tile, s);
+    int st = gemm<T, false, true, DACT>(P, plan(DACT, d.e, d.rows, d.F, d.O, 1).tile, s, d.act);
     if (st) return st;
     const Plan p = dx_plan(d);
     FfnParams R{};
@@ -501,19 +597,29 @@ int dgrad(const Desc& d, const void* dy, const void* w1, const void* w2, const v
     if (p.splits == 1) return gemm<T, false, true, STORE>(R, p.tile, s);
     st = gemm<T, false, true, PART>(R, p.tile, s);
     if (st) return st;
-    const long long n = d.rows * d.C;
-    ffn_add_parts_kernel<T><<<(unsigned)tiles_of(n, 256), 256, 0, s>>>((const float*)ws, (T*)dx, n, p.splits);
-    return check_launch();
+    return add_parts<T>((const float*)ws, (T*)dx, d.rows * d.C, nullptr, nullptr, 0, p.splits, s);
 }
-// out[m][n] = sum over rows of a[row][m] b[row][n]
 template <typename T>
-int outer(const void* a, const void* b, long long rows, int M, int N, float* out, void* ws, hipStream_t s) {
-    const Plan p = outer_plan(rows, M, N, sizeof(T));
-    FfnParams P{};
-    P.q = a; P.p = b; P.M = M; P.K = rows; P.N = N; P.qp = M; P.pp = N; P.splits = p.splits;
-    P.out = p.splits > 1 ? ws : out;
-    const int st = gemm<T, true, true, PART>(P, p.tile, s);
-    return st || p.splits == 1 ? st : reduce_partials((const float*)ws, out, (long long)M * N, p.splits, s);
+int wgrad(const Desc& d, const void* x, const void* dgu, const void* h, const void* dy, float* dw1, float* dw2, void* ws, hipStream_t s) {
+    const WgradPlan p = wgrad_plan(d);
+    const long long n1 = 2ll * d.F * d.C, n2 = (long long)d.O * d.F;
+    float* parts = (float*)ws;
+    FfnPair P{};
+    P.a.q = dgu; P.a.p = x; P.a.M = 2 * d.F; P.a.K = d.rows; P.a.N = d.C; P.a.qp = 2 * d.F; P.a.pp = d.C; P.a.splits = p.first.splits;
+    P.b.q = dy; P.b.p = h; P.b.M = d.O; P.b.K = d.rows; P.b.N = d.F; P.b.qp = d.O; P.b.pp = d.F; P.b.splits = p.second.splits;
+    P.a.out = p.first.splits > 1 ? parts : dw1;
+    P.b.out = p.second.splits > 1 ? parts + (p.pair ? p.first.splits * n1 : 0) : dw2;
+    int st;
+    if (!p.pair) {
+        st = gemm<T, true, true, PART>(P.a, p.first.tile, s);
+        if (!st && p.first.splits > 1) st = add_parts<float>(parts, dw1, n1, nullptr, nullptr, 0, p.first.splits, s);
+        if (!st) st = gemm<T, true, true, PART>(P.b, p.second.tile, s);
+        return st || p.second.splits == 1 ? st : add_parts<float>(parts, dw2, n2, nullptr, nullptr, 0, p.second.splits, s);
+    }
+    if (sizeof(T) == 2 && p.first.tile == LARGE) st = launch_pair<uint16_t, 4, 2, 4, 64, 4>(P, s);
+    else if (p.first.tile == MIDDLE) st = launch_pair<T, 2, 2, 2, 128, 2>(P, s);
+    else st = launch_pair<T, 1, 2, 2, 128, 3>(P, s);
+    return st || p.first.splits == 1 ? st : add_parts<float>(parts, dw1, n1, parts + p.first.splits * n1, dw2, n2, p.first.splits, s);
 }
 
 }  // namespace
@@ -569,16 +675,14 @@ int mi3d_ffn_dgrad(const mi3d_ffn_desc* desc, const void* dy, const void* w1, co
 int mi3d_ffn_wgrad(const mi3d_ffn_desc* desc, const void* x, const void* dgu, const void* h, const void* dy, float* dw1, float* dw2,
                    void* ws, size_t ws_bytes, void* stream) {
     Desc d;
-    int st = make(desc, &d);
+    const int st = make(desc, &d);
     if (st) return st;
     if (!usable(dw1) || !usable(dw2) || !aligned16(x) || !aligned16(dgu) || !aligned16(h) || !aligned16(dy) || !aligned16(ws)) return MI3D_ERR_INVALID_ARG;
     if (d.rows && (!x || !dgu || !h || !dy)) return MI3D_ERR_INVALID_ARG;
     const size_t need = workspace(d, MI3D_PASS_WGRAD);
     if (need && (!ws || ws_bytes < need)) return MI3D_ERR_WORKSPACE;
     const hipStream_t s = (hipStream_t)stream;
-    st = d.e == 2 ? outer<uint16_t>(dgu, x, d.rows, 2 * d.F, d.C, dw1, ws, s) : outer<float>(dgu, x, d.rows, 2 * d.F, d.C, dw1, ws, s);
-    if (st) return st;
-    return d.e == 2 ? outer<uint16_t>(dy, h, d.rows, d.O, d.F, dw2, ws, s) : outer<float>(dy, h, d.rows, d.O, d.F, dw2, ws, s);
+    return d.e == 2 ? wgrad<uint16_t>(d, x, dgu, h, dy, dw1, dw2, ws, s) : wgrad<float>(d, x, dgu, h, dy, dw1, dw2, ws, s);
 }
 
 }  // extern "C"

@@ -27,9 +27,9 @@ __device__ __forceinline__ f32x4 product(const uint4& w, const uint4& x, f32x4 c
 }
 
 // NB blocks of 16 rows of x; U pieces of 128 bytes of k requested ahead of their products
-template <typename T, int NB, bool GATED, int U>
+template <typename T, int NB, bool GATED, int ACT, int U>
 __global__ void __launch_bounds__(512) few_rows_kernel(const T* __restrict__ x, const T* __restrict__ w, long long rows, int K, int N,
-                                                        int act, T* __restrict__ out, T* __restrict__ gu) {
+                                                        T* __restrict__ out, T* __restrict__ gu) {
     constexpr int G = GATED ? 2 : 1, E = sizeof(T), PIECE = 128 / E;
     extern __shared__ f32x4 sums[];      // [wave][G * NB][lane]
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, W = blockDim.x >> 6;
@@ -100,7 +100,7 @@ __global__ void __launch_bounds__(512) few_rows_kernel(const T* __restrict__ x, 
                 put(gu + (long long)m * 2 * N + N + n, v[1]);
             }
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[0][j] = activation<T>(v[0][j], act) * v[1][j];
+            for (int j = 0; j < 4; ++j) v[0][j] = activation<T, ACT>(v[0][j]) * v[1][j];
         }
         put(out + (long long)m * N + n, v[0]);
     }
@@ -134,18 +134,23 @@ int few_rows_product(bool bf16, bool gated, const void* x, const void* w, long l
     const size_t lds = (size_t)W * (gated ? 2 : 1) * nb * 1024;
     auto go = [&](auto type, auto kernel) {
         typedef decltype(type) T;
-        kernel<<<grid, 64 * W, lds, s>>>((const T*)x, (const T*)w, rows, K, N, act, (T*)out, (T*)gu);
+        kernel<<<grid, 64 * W, lds, s>>>((const T*)x, (const T*)w, rows, K, N, (T*)out, (T*)gu);
     };
+    constexpr int SILU = MI3D_ACT_SILU, GELU = MI3D_ACT_GELU;
     auto pick = [&](auto type) {
         typedef decltype(type) T;
-        if (gated) {
-            if (nb == 1) go(type, few_rows_kernel<T, 1, true, 4>);
-            else if (nb == 2) go(type, few_rows_kernel<T, 2, true, 2>);
-            else go(type, few_rows_kernel<T, 4, true, 1>);
+        if (!gated) {
+            if (nb == 1) go(type, few_rows_kernel<T, 1, false, SILU, 4>);
+            else if (nb == 2) go(type, few_rows_kernel<T, 2, false, SILU, 2>);
+            else go(type, few_rows_kernel<T, 4, false, SILU, 2>);
+        } else if (act == SILU) {
+            if (nb == 1) go(type, few_rows_kernel<T, 1, true, SILU, 4>);
+            else if (nb == 2) go(type, few_rows_kernel<T, 2, true, SILU, 2>);
+            else go(type, few_rows_kernel<T, 4, true, SILU, 1>);
         } else {
-            if (nb == 1) go(type, few_rows_kernel<T, 1, false, 4>);
-            else if (nb == 2) go(type, few_rows_kernel<T, 2, false, 2>);
-            else go(type, few_rows_kernel<T, 4, false, 2>);
+            if (nb == 1) go(type, few_rows_kernel<T, 1, true, GELU, 4>);
+            else if (nb == 2) go(type, few_rows_kernel<T, 2, true, GELU, 2>);
+            else go(type, few_rows_kernel<T, 4, true, GELU, 1>);
         }
     };
     if (bf16) pick(uint16_t{});

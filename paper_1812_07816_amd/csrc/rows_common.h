@@ -38,6 +38,18 @@ __device__ __forceinline__ void store_values(T* p, const float (&f)[V]) {
         ((float4*)p)[1] = float4{f[4], f[5], f[6], f[7]};
     }
 }
+// the same for 8 values that stay out of the way of what is read again soon
+template <typename T>
+__device__ __forceinline__ void store_streamed(T* p, const float (&f)[8]) {
+    typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t u32x4;
+    typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4;
+    if constexpr (sizeof(T) == 2) {
+        __builtin_nontemporal_store(u32x4{pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7])}, (u32x4*)p);
+    } else {
+        __builtin_nontemporal_store(f32x4{f[0], f[1], f[2], f[3]}, (f32x4*)p);
+        __builtin_nontemporal_store(f32x4{f[4], f[5], f[6], f[7]}, (f32x4*)p + 1);
+    }
+}
 inline bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
 }  // namespace mi3d
