@@ -403,6 +403,9 @@ typedef struct {
     int dtype; /* mi3d_dtype */
 } mi3d_ffn_desc;
 size_t mi3d_ffn_workspace_bytes(const mi3d_ffn_desc *desc, int pass);
+/* The kernels that a call runs, for reports and tests: its tiles for each product, and the parts of the contraction
+ * ("tiles_128x128, few_rows parts 1", "pair tiles_64x128 parts 6"). */
+int mi3d_ffn_kernel_detail(const mi3d_ffn_desc *desc, int pass, char *buf, size_t buf_len);
 /* The first half: both projections, the activation and the product.  gu may be NULL (inference, or a block that computes it
  * again in the backward pass with this call).  h is formed from the fp32 sums, gu holds them rounded. */
 int mi3d_ffn_gate(const mi3d_ffn_desc *desc, const void *x, const void *w1, void *h, void *gu, void *stream);

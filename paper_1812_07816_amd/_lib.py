@@ -87,6 +87,7 @@ SIGNATURES = {
     "mi3d_dropout_channels": (_i, [_vp, _vp, _i, _sz, _i, _f, _u64, _u64, _vp, _vp]),
     "mi3d_dropout_channels_f32": (_i, [_vp, _vp, _i, _sz, _i, _f, _u64, _u64, _vp, _vp]),
     "mi3d_ffn_workspace_bytes": (_sz, [_pf, _i]),
+    "mi3d_ffn_kernel_detail": (_i, [_pf, _i, ctypes.c_char_p, _sz]),
     "mi3d_ffn_gate": (_i, [_pf, _vp, _vp, _vp, _vp, _vp]),
     "mi3d_ffn_fwd": (_i, [_pf, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
     "mi3d_ffn_dgrad": (_i, [_pf, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),

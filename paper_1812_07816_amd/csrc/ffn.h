@@ -38,7 +38,7 @@ __device__ __forceinline__ float activation(float g) {
 // The forward products of few rows, or of small matrices.  gated: w holds 2 N rows, out = act(g) * u (and [g | u] where gu is not
 // null); otherwise N rows and out = x w^T.  K and N are multiples of 8.  few_rows_us: what its model expects it to take (very long:
 // too many rows).
-double few_rows_us(bool bf16, bool gated, long long rows, long long K, long long N);
+double few_rows_us(bool bf16, long long rows, long long K, long long N);
 int few_rows_product(bool bf16, bool gated, const void* x, const void* w, long long rows, int K, int N, int act, void* out, void* gu, hipStream_t s);
 
 }  // namespace mi3d

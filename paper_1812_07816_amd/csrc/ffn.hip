@@ -10,6 +10,8 @@
 // instruction, whose results a lane then holds as four neighbouring n of one row.  bf16: v_mfma_f32_32x32x16_bf16; fp32:
 // v_mfma_f32_32x32x2_f32 on the same 16-byte pieces, four of k.  Sums in fp32.  Bound: the matrix instructions.
 
+#include <cstdio>
+
 #include "ffn.h"
 #include "ig_common.h"
 
@@ -443,8 +445,8 @@ double tiles_us(const TileTimes& t, bool dact, long long tiles, double steps) {
     const double fixed = dact ? t.dact : t.fixed;
     return (double)(tiles / slots) * (fixed + steps * t.shared) + (rest == 0 ? 0.0 : rest <= cus ? fixed + steps * t.alone : fixed + steps * t.shared);
 }
-// time of adding the parts of n sums
-double add_us(int splits, double n) { return splits > 1 ? 3.0 + (splits + 1.0) * 4.0 * n / 5e6 : 0.0; }
+// time of adding the parts of n sums, with the launch
+double add_us(int splits, double n) { return splits > 1 ? 5.0 + (splits + 1.0) * 4.0 * n / 5e6 : 0.0; }
 // cols: columns of D that tiles cover (GATE: of both halves).  most_parts 1: the contraction is not split.  M2 x cols2: a second product
 // with the same contraction in the same launch
 Plan plan(Form form, int e, long long M, long long cols, long long K, int most_parts, long long M2 = 0, long long cols2 = 0) {
@@ -459,7 +461,7 @@ Plan plan(Form form, int e, long long M, long long cols, long long K, int most_p
         }
     }
     if (form == GATE || form == STORE) {
-        const double us = few_rows_us(e == 2, form == GATE, M, K, form == GATE ? cols / 2 : cols);
+        const double us = few_rows_us(e == 2, M, K, form == GATE ? cols / 2 : cols);
         if (us < best.us) best = Plan{FEW, 1, us};
     }
     return best;
@@ -541,67 +543,90 @@ int make(const mi3d_ffn_desc* d, Desc* o) {
     return MI3D_OK;
 }
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
-Plan dx_plan(const Desc& d) { return plan(PART, d.e, d.rows, d.C, 2 * d.F, MOST_PARTS); }
-// Both weight gradients in one launch, or one after the other with parts of their own (16384 x 1024 x 4096: 427 us together, 368 apart;
-// 27000 x 256 x 1024: 68 and 76)
-struct WgradPlan {
-    bool pair;
+// The plans of a pass.  pair: both weight gradients in one launch, else one after the other with parts of their own (16384 x 1024 x 4096:
+// 427 us together, 368 apart; 27000 x 256 x 1024: 68 and 76)
+struct Plans {
     Plan first, second;
+    bool pair;
 };
-WgradPlan wgrad_plan(const Desc& d) {
+Plans make_plans(const Desc& d, int pass) {
+    if (pass == MI3D_PASS_FWD) return Plans{plan(GATE, d.e, d.rows, 2 * d.F, d.C, 1), plan(STORE, d.e, d.rows, d.O, d.F, MOST_PARTS), false};
+    if (pass == MI3D_PASS_DGRAD) return Plans{plan(DACT, d.e, d.rows, d.F, d.O, 1), plan(PART, d.e, d.rows, d.C, 2 * d.F, MOST_PARTS), false};
     const Plan both = plan(PART, d.e, 2 * d.F, d.C, d.rows, MOST_PARTS, d.O, d.F);
     const Plan first = plan(PART, d.e, 2 * d.F, d.C, d.rows, MOST_PARTS), second = plan(PART, d.e, d.O, d.F, d.rows, MOST_PARTS);
-    if (both.us <= first.us + second.us) return WgradPlan{true, both, both};
-    return WgradPlan{false, first, second};
+    if (both.us <= first.us + second.us + 3.0) return Plans{both, both, true};
+    return Plans{first, second, false};
+}
+// A call asks twice (its workspace, its kernels) and the weighing takes 1 to 3 us, a quarter of what one row takes in all: a thread keeps
+// the last ones, by everything that they depend on.
+Plans plans_of(const Desc& d, int pass) {
+    struct Slot {
+        long long rows;
+        int C, F, O, e, pass, cus;
+        Plans plans;
+    };
+    static thread_local Slot slots[16];      // (C = 0: none)
+    const int cus = cu_count();
+    uint64_t h = (uint64_t)d.rows * 3 + pass;
+    for (int v : {d.C, d.F, d.O, d.e}) h = h * 0x9E3779B97F4A7C15ull + (uint32_t)v;
+    Slot& s = slots[h * 0x9E3779B97F4A7C15ull >> 60];
+    if (s.rows != d.rows || s.C != d.C || s.F != d.F || s.O != d.O || s.e != d.e || s.pass != pass || s.cus != cus)
+        s = Slot{d.rows, d.C, d.F, d.O, d.e, pass, cus, make_plans(d, pass)};
+    return s.plans;
 }
 size_t parts_bytes(int splits, long long M, long long N) { return splits > 1 ? (size_t)splits * M * N * 4 : 0; }
 bool usable(const void* p) { return p && aligned16(p); }
 
 size_t workspace(const Desc& d, int pass) {
-    if (pass == MI3D_PASS_FWD) return round256((size_t)d.rows * d.F * d.e);      // h
-    if (pass == MI3D_PASS_DGRAD) return d.rows ? parts_bytes(dx_plan(d).splits, d.rows, d.C) : 0;
+    if (pass == MI3D_PASS_FWD) return d.rows ? round256((size_t)d.rows * d.F * d.e) + parts_bytes(plans_of(d, pass).second.splits, d.rows, d.O) : 0;      // h, parts of y
+    if (pass == MI3D_PASS_DGRAD) return d.rows ? parts_bytes(plans_of(d, pass).second.splits, d.rows, d.C) : 0;
     if (pass != MI3D_PASS_WGRAD) return 0;
-    const WgradPlan p = wgrad_plan(d);
+    const Plans p = plans_of(d, pass);
     const size_t n1 = parts_bytes(p.first.splits, 2 * d.F, d.C), n2 = parts_bytes(p.second.splits, d.O, d.F);
     return p.pair ? n1 + n2 : n1 > n2 ? n1 : n2;
 }
 
 template <typename T>
 int gate(const Desc& d, const void* x, const void* w1, void* h, void* gu, hipStream_t s) {
-    const Plan p = plan(GATE, d.e, d.rows, 2 * d.F, d.C, 1);
+    const Plan p = plans_of(d, MI3D_PASS_FWD).first;
     if (p.tile == FEW) return few_rows_product(sizeof(T) == 2, true, x, w1, d.rows, d.C, d.F, d.act, h, gu, s);
     FfnParams P{};
     P.q = x; P.p = w1; P.M = d.rows; P.K = d.C; P.N = d.F; P.qp = d.C; P.pp = d.C; P.F = d.F;
     P.out = h; P.out2 = gu;
     return gemm<T, false, false, GATE>(P, p.tile, s, d.act);
 }
+// D of P's operands, by way of its parts where the plan has some
+template <typename T, bool PA>
+int rows_product(FfnParams P, const Plan& p, void* out, void* parts, hipStream_t s) {
+    P.splits = p.splits;
+    P.out = p.splits > 1 ? parts : out;
+    if (p.splits == 1) return gemm<T, false, PA, STORE>(P, p.tile, s);
+    const int st = gemm<T, false, PA, PART>(P, p.tile, s);
+    return st ? st : add_parts<T>((const float*)parts, (T*)out, P.M * P.N, nullptr, nullptr, 0, p.splits, s);
+}
 template <typename T>
-int project(const Desc& d, const void* h, const void* w2, void* y, hipStream_t s) {
-    const Plan p = plan(STORE, d.e, d.rows, d.O, d.F, 1);
-    if (p.tile == FEW) return few_rows_product(sizeof(T) == 2, false, h, w2, d.rows, d.F, d.O, 0, y, nullptr, s);
+int project(const Desc& d, void* ws, const void* w2, void* y, hipStream_t s) {
+    const Plan p = plans_of(d, MI3D_PASS_FWD).second;
+    if (p.tile == FEW) return few_rows_product(sizeof(T) == 2, false, ws, w2, d.rows, d.F, d.O, 0, y, nullptr, s);
     FfnParams P{};
-    P.q = h; P.p = w2; P.M = d.rows; P.K = d.F; P.N = d.O; P.qp = d.F; P.pp = d.F; P.out = y;
-    return gemm<T, false, false, STORE>(P, p.tile, s);
+    P.q = ws; P.p = w2; P.M = d.rows; P.K = d.F; P.N = d.O; P.qp = d.F; P.pp = d.F;
+    return rows_product<T, false>(P, p, y, (char*)ws + round256((size_t)d.rows * d.F * d.e), s);
 }
 template <typename T>
 int dgrad(const Desc& d, const void* dy, const void* w1, const void* w2, const void* gu, void* dgu, void* h, void* dx, void* ws, hipStream_t s) {
     FfnParams P{};
     P.q = dy; P.p = w2; P.M = d.rows; P.K = d.O; P.N = d.F; P.qp = d.O; P.pp = d.F;
     P.out = h; P.out2 = dgu; P.gu = gu;
-    int st = gemm<T, false, true, DACT>(P, plan(DACT, d.e, d.rows, d.F, d.O, 1).tile, s, d.act);
+    const Plans p = plans_of(d, MI3D_PASS_DGRAD);
+    const int st = gemm<T, false, true, DACT>(P, p.first.tile, s, d.act);
     if (st) return st;
-    const Plan p = dx_plan(d);
     FfnParams R{};
-    R.q = dgu; R.p = w1; R.M = d.rows; R.K = 2 * d.F; R.N = d.C; R.qp = 2 * d.F; R.pp = d.C; R.splits = p.splits;
-    R.out = p.splits > 1 ? ws : dx;
-    if (p.splits == 1) return gemm<T, false, true, STORE>(R, p.tile, s);
-    st = gemm<T, false, true, PART>(R, p.tile, s);
-    if (st) return st;
-    return add_parts<T>((const float*)ws, (T*)dx, d.rows * d.C, nullptr, nullptr, 0, p.splits, s);
+    R.q = dgu; R.p = w1; R.M = d.rows; R.K = 2 * d.F; R.N = d.C; R.qp = 2 * d.F; R.pp = d.C;
+    return rows_product<T, true>(R, p.second, dx, ws, s);
 }
 template <typename T>
 int wgrad(const Desc& d, const void* x, const void* dgu, const void* h, const void* dy, float* dw1, float* dw2, void* ws, hipStream_t s) {
-    const WgradPlan p = wgrad_plan(d);
+    const Plans p = plans_of(d, MI3D_PASS_WGRAD);
     const long long n1 = 2ll * d.F * d.C, n2 = (long long)d.O * d.F;
     float* parts = (float*)ws;
     FfnPair P{};
@@ -632,6 +657,20 @@ extern "C" {
 size_t mi3d_ffn_workspace_bytes(const mi3d_ffn_desc* desc, int pass) {
     Desc d;
     return make(desc, &d) == MI3D_OK ? workspace(d, pass) : 0;
+}
+
+int mi3d_ffn_kernel_detail(const mi3d_ffn_desc* desc, int pass, char* buf, size_t buf_len) {
+    Desc d;
+    const int st = make(desc, &d);
+    if (st) return st;
+    if (!buf || !buf_len || pass < MI3D_PASS_FWD || pass > MI3D_PASS_WGRAD) return MI3D_ERR_INVALID_ARG;
+    static const char* const names[4] = {"tiles_256x256", "tiles_128x128", "tiles_64x128", "few_rows"};
+    const Plans p = plans_of(d, pass);
+    const char *first = names[p.first.tile], *second = names[p.second.tile];
+    if (pass != MI3D_PASS_WGRAD) snprintf(buf, buf_len, "%s, %s parts %d", first, second, p.second.splits);
+    else if (p.pair) snprintf(buf, buf_len, "pair %s parts %d", first, p.first.splits);
+    else snprintf(buf, buf_len, "%s parts %d, %s parts %d", first, p.first.splits, second, p.second.splits);
+    return MI3D_OK;
 }
 
 int mi3d_ffn_gate(const mi3d_ffn_desc* desc, const void* x, const void* w1, void* h, void* gu, void* stream) {

@@ -117,12 +117,14 @@ static int blocks_of(long long rows, int N) {
     return nb;
 }
 
-// What it is expected to take: microseconds for every 128 bytes of k that a compute unit goes through, measured on the sizes above
-double few_rows_us(bool bf16, bool gated, long long rows, long long K, long long N) {
+// What it is expected to take, in microseconds: for every workgroup of a compute unit a fixed time and one for each 128 bytes of k, measured
+// with 1, 2 and 4 blocks of rows on the sizes above and one row of 1024 and 4096
+double few_rows_us(bool bf16, long long rows, long long K, long long N) {
     const int nb = blocks_of(rows, (int)N);
     const double groups = (double)((N + 15) / 16) * (double)((rows + 16 * nb - 1) / (16 * nb)) / cu_count(), pieces = (double)((K * (bf16 ? 2 : 4) + 127) / 128);
     if ((rows + 16 * nb - 1) / (16 * nb) > 65535) return 1e30;
-    return 3.5 + (groups < 1.0 ? 1.0 : groups) * pieces * (bf16 ? 0.4 : 0.65) * (nb == 4 ? 1.0 : nb == 2 ? 0.63 : 0.42);
+    static constexpr double each[2][3] = {{0.12, 0.30, 0.60}, {0.09, 0.22, 0.40}};
+    return 3.5 + (groups < 1.0 ? 1.0 : groups) * ((bf16 ? 0.2 : 0.8) + pieces * each[bf16][nb / 2]);
 }
 
 int few_rows_product(bool bf16, bool gated, const void* x, const void* w, long long rows, int K, int N, int act, void* out, void* gu, hipStream_t s) {

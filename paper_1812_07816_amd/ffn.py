@@ -27,6 +27,13 @@ def workspace(desc, pass_):
     return torch.empty(max(workspace_bytes(desc, pass_), 16), dtype=torch.uint8, device="cuda")
 
 
+def kernel_detail(desc, pass_):
+    """The kernels that a call runs."""
+    buf = ctypes.create_string_buffer(128)
+    check(lib().mi3d_ffn_kernel_detail(ctypes.byref(desc), pass_, buf, 128), "ffn_kernel_detail")
+    return buf.value.decode()
+
+
 def _chk(dev, rows, C, dtype, **tensors):
     """Refuses what is not a dense tensor of rows x C values of this type on this device (None: left out)."""
     for name, t in tensors.items():
