@@ -348,7 +348,7 @@ int mi3d_adam_update(float *w, const float *dw, float *m, float *v, void *w_bf16
 /* Layer normalisation of each row over its C channels, with scale gamma and shift beta (C floats each):
  * xhat = (x - mean) * rstd, rstd = 1 / sqrt(var + eps) with the biased variance, y = gamma * xhat + beta.
  * stats (may be NULL; 8-byte aligned): (mean, rstd) of each row, 2 * rows floats, for the backward pass.  y may be x.
- * C <= 16384 in multiples of 8, any other C <= 2048; others and 2^40 rows return MI3D_ERR_UNSUPPORTED. */
+ * C <= 16384 (multiples of 8 are fastest); wider rows and 2^40 of them return MI3D_ERR_UNSUPPORTED. */
 int mi3d_layernorm_fwd(const void *x, const float *gamma, const float *beta, size_t rows, int C, float eps, void *y,
                        float *stats, void *stream);
 int mi3d_layernorm_fwd_f32(const void *x, const float *gamma, const float *beta, size_t rows, int C, float eps, void *y,

@@ -3,10 +3,10 @@
 // Backward, from x and the row's (mean, rstd), with g = dy * gamma:
 //   dx = rstd * (g - mean_c(g) - xhat * mean_c(g * xhat)) (+ add),  dgamma = sum_rows dy * xhat,  dbeta = sum_rows dy.
 //
-// Bound: HBM.  A row stays in the registers of L lanes, K pieces of V values each, so that it is read once and the
+// Bound: HBM.  A row stays in the registers of L lanes, K pieces of eight values each, so that it is read once and the
 // variance is a sum of squared differences from the mean (no cancellation where the mean is large); sums in fp32.  The
 // sums over rows are kept per lane (a lane always has the same channels), added over the lanes of a workgroup in lane
-// order, and over the workgroups in double in index order by a second launch (bit-reproducible).
+// order, and over the workgroups in double in a fixed order by a second launch (bit-reproducible).
 #include "mi3d_internal.h"
 #include "rows_common.h"
 
@@ -28,30 +28,58 @@ __device__ __forceinline__ float row_sum(float v, int L, float* red) {
     return v;
 }
 
-template <typename T, int V, int K>
-__global__ void __launch_bounds__(512) ln_fwd_kernel(const T* __restrict__ x, const float* __restrict__ gamma, const float* __restrict__ beta,
+// How a row lies in pieces: EVEN: C in multiples of 8, aligned pieces of 8.  ODD: any other C from 8 on, pieces of 8 at any address, the
+// last of them moved back to end with the row, so that its first `skip` values are the last ones of the piece before and count
+// there (both lanes store the same).  TINY: C below 8, one value at a time.
+enum Form { EVEN, ODD, TINY };
+template <Form F> constexpr int V = F == TINY ? 1 : 8;
+struct Place {
+    int col, skip;
+    __device__ __forceinline__ bool counts(int j) const { return j >= skip; }
+};
+template <Form F>
+__device__ __forceinline__ Place place(int piece, int C) {
+    const int at = piece * V<F>;
+    if (F != ODD || at + 8 <= C) return Place{at, 0};
+    return Place{C - 8, at + 8 - C};
+}
+template <Form F, typename T>
+__device__ __forceinline__ void get(const T* p, float (&f)[V<F>]) {
+    if constexpr (F == ODD) load8_anywhere(p, f);
+    else load_values<T, V<F>>(p, f);
+}
+template <Form F, typename T>
+__device__ __forceinline__ void put(T* p, const float (&f)[V<F>]) {
+    if constexpr (F == ODD) store8_anywhere(p, f);
+    else store_values<T, V<F>>(p, f);
+}
+
+template <typename T, Form F, int K>
+__global__ void __launch_bounds__(512) ln_fwd_kernel(const T* x, const float* __restrict__ gamma, const float* __restrict__ beta,
                                                      T* y, float2* __restrict__ stats, long long rows, int C, int L, float eps) {
     __shared__ float red[16];
-    const int l = threadIdx.x & (L - 1), mine = threadIdx.x / L, per = blockDim.x / L, P = C / V;
+    const int l = threadIdx.x & (L - 1), mine = threadIdx.x / L, per = blockDim.x / L, P = (C + V<F> - 1) / V<F>;
     const float inv = 1.f / (float)C;
-    float ga[K][V], be[K][V];
+    float ga[K][V<F>], be[K][V<F>];
+    Place at[K];
 #pragma unroll
     for (int k = 0; k < K; ++k)
         if (l + k * L < P) {
-            load_values<float, V>(gamma + (l + k * L) * V, ga[k]);
-            load_values<float, V>(beta + (l + k * L) * V, be[k]);
+            at[k] = place<F>(l + k * L, C);
+            get<F>(gamma + at[k].col, ga[k]);
+            get<F>(beta + at[k].col, be[k]);
         }
     const long long step = (long long)gridDim.x * per;
     // (the lanes of a workgroup take the same number of turns: row_sum may wait for all of them)
     for (long long r0 = (long long)blockIdx.x * per; r0 < rows; r0 += step) {
         const long long r = r0 + mine;
-        float v[K][V] = {}, s = 0.f;
+        float v[K][V<F>] = {}, s = 0.f;
 #pragma unroll
         for (int k = 0; k < K; ++k)
             if (r < rows && l + k * L < P) {
-                load_values<T, V>(x + r * C + (l + k * L) * V, v[k]);
+                get<F>(x + r * C + at[k].col, v[k]);
 #pragma unroll
-                for (int j = 0; j < V; ++j) s += v[k][j];
+                for (int j = 0; j < V<F>; ++j) s += F != ODD || at[k].counts(j) ? v[k][j] : 0.f;
             }
         const float mean = row_sum(s, L, red) * inv;
         s = 0.f;
@@ -59,76 +87,80 @@ __global__ void __launch_bounds__(512) ln_fwd_kernel(const T* __restrict__ x, co
         for (int k = 0; k < K; ++k)
             if (l + k * L < P)
 #pragma unroll
-                for (int j = 0; j < V; ++j) {
+                for (int j = 0; j < V<F>; ++j) {
                     v[k][j] -= mean;
-                    s = fmaf(v[k][j], v[k][j], s);
+                    const float d = F != ODD || at[k].counts(j) ? v[k][j] : 0.f;
+                    s = fmaf(d, d, s);
                 }
         const float rstd = 1.f / sqrtf(row_sum(s, L, red + 8) * inv + eps);
         if (r >= rows) continue;
 #pragma unroll
         for (int k = 0; k < K; ++k)
             if (l + k * L < P) {
-                float o[V];
+                float o[V<F>];
 #pragma unroll
-                for (int j = 0; j < V; ++j) o[j] = fmaf(v[k][j] * rstd, ga[k][j], be[k][j]);
-                store_values<T, V>(y + r * C + (l + k * L) * V, o);
+                for (int j = 0; j < V<F>; ++j) o[j] = fmaf(v[k][j] * rstd, ga[k][j], be[k][j]);
+                put<F>(y + r * C + at[k].col, o);
             }
         if (l == 0 && stats) stats[r] = float2{mean, rstd};
     }
 }
 
 // part: [workgroup][2][C], the workgroup's sums of dy * xhat and of dy
-template <typename T, int V, int K>
+template <typename T, Form F, int K>
 __global__ void __launch_bounds__(512) ln_bwd_kernel(const T* dy, const T* x, const float2* __restrict__ stats, const float* __restrict__ gamma,
                                                      const T* add, T* dx, float* __restrict__ part, long long rows, int C, int L) {
     extern __shared__ float sums[];      // [rows of a turn][C]
     __shared__ float red[16];
-    const int l = threadIdx.x & (L - 1), mine = threadIdx.x / L, per = blockDim.x / L, P = C / V;
+    const int l = threadIdx.x & (L - 1), mine = threadIdx.x / L, per = blockDim.x / L, P = (C + V<F> - 1) / V<F>;
     const float inv = 1.f / (float)C;
-    float ga[K][V], dg[K][V], db[K][V];
+    float ga[K][V<F>], dg[K][V<F>] = {}, db[K][V<F>] = {};
+    Place at[K];
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-        if (l + k * L < P) load_values<float, V>(gamma + (l + k * L) * V, ga[k]);
-#pragma unroll
-        for (int j = 0; j < V; ++j) dg[k][j] = db[k][j] = 0.f;
-    }
+    for (int k = 0; k < K; ++k)
+        if (l + k * L < P) {
+            at[k] = place<F>(l + k * L, C);
+            get<F>(gamma + at[k].col, ga[k]);
+        }
     const long long step = (long long)gridDim.x * per;
     for (long long r0 = (long long)blockIdx.x * per; r0 < rows; r0 += step) {
         const long long r = r0 + mine;
-        float xh[K][V] = {}, g[K][V] = {}, s1 = 0.f, s2 = 0.f;
+        float xh[K][V<F>] = {}, g[K][V<F>] = {}, s1 = 0.f, s2 = 0.f;
         float2 st = {0.f, 0.f};
         if (r < rows) st = stats[r];
 #pragma unroll
         for (int k = 0; k < K; ++k)
             if (r < rows && l + k * L < P) {
-                load_values<T, V>(x + r * C + (l + k * L) * V, xh[k]);
-                load_values<T, V>(dy + r * C + (l + k * L) * V, g[k]);
+                get<F>(x + r * C + at[k].col, xh[k]);
+                get<F>(dy + r * C + at[k].col, g[k]);
 #pragma unroll
-                for (int j = 0; j < V; ++j) {
+                for (int j = 0; j < V<F>; ++j) {
                     xh[k][j] = (xh[k][j] - st.x) * st.y;
                     dg[k][j] = fmaf(g[k][j], xh[k][j], dg[k][j]);
                     db[k][j] += g[k][j];
                     g[k][j] *= ga[k][j];
-                    s1 += g[k][j];
-                    s2 = fmaf(g[k][j], xh[k][j], s2);
+                    const float d = F != ODD || at[k].counts(j) ? g[k][j] : 0.f;
+                    s1 += d;
+                    s2 = F != ODD || at[k].counts(j) ? fmaf(d, xh[k][j], s2) : s2;
                 }
             }
         const float m1 = row_sum(s1, L, red) * inv, m2 = row_sum(s2, L, red + 8) * inv;
+        // (an ODD row's pieces overlap: none is stored before all are read, add's among them, which dx may be)
+        float a[K][V<F>] = {};
+        if (add && r < rows) {
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+                if (l + k * L < P) get<F>(add + r * C + at[k].col, a[k]);
+        }
+        if (F == ODD && L > 64) __syncthreads();
         if (r >= rows) continue;
 #pragma unroll
         for (int k = 0; k < K; ++k)
             if (l + k * L < P) {
-                const long long at = r * C + (l + k * L) * V;
-                float o[V];
+                float o[V<F>];
 #pragma unroll
-                for (int j = 0; j < V; ++j) o[j] = st.y * (g[k][j] - m1 - xh[k][j] * m2);
-                if (add) {
-                    float a[V];
-                    load_values<T, V>(add + at, a);
-#pragma unroll
-                    for (int j = 0; j < V; ++j) o[j] += a[j];
-                }
-                store_values<T, V>(dx + at, o);
+                for (int j = 0; j < V<F>; ++j) o[j] = st.y * (g[k][j] - m1 - xh[k][j] * m2) + a[k][j];
+                put<F>(dx + r * C + at[k].col, o);
             }
     }
     float* out = part + (long long)blockIdx.x * 2 * C;
@@ -138,7 +170,8 @@ __global__ void __launch_bounds__(512) ln_bwd_kernel(const T* dy, const T* x, co
         for (int k = 0; k < K; ++k)
             if (l + k * L < P)
 #pragma unroll
-                for (int j = 0; j < V; ++j) (per > 1 ? sums + mine * C : out + q * C)[(l + k * L) * V + j] = q ? db[k][j] : dg[k][j];
+                for (int j = 0; j < V<F>; ++j)
+                    if (F != ODD || at[k].counts(j)) (per > 1 ? sums + mine * C : out + q * C)[at[k].col + j] = q ? db[k][j] : dg[k][j];
         __syncthreads();
         if (per > 1)
             for (int c = threadIdx.x; c < C; c += blockDim.x) {
@@ -149,42 +182,56 @@ __global__ void __launch_bounds__(512) ln_bwd_kernel(const T* dy, const T* x, co
     }
 }
 
-// dgamma, dbeta from the workgroups' sums: 16 columns a workgroup, thread (slice, column) adds parts slice, slice + 16, ...
-__global__ void __launch_bounds__(256) ln_finish_kernel(const float* __restrict__ part, int parts, int C, float* __restrict__ dgamma, float* __restrict__ dbeta) {
-    __shared__ double red[16][17];
+// dgamma, dbeta from the workgroups' sums: 16 columns a workgroup, thread (slice, column) adds parts slice, slice + 64, ... in double, and the
+// slices are added in order.  Bound: the latency of the loads, of which four are under way (27648 x 320, 864 parts: 25 us with 16
+// slices and one load at a time).
+__global__ void __launch_bounds__(1024) ln_finish_kernel(const float* __restrict__ part, int parts, int C, float* __restrict__ dgamma, float* __restrict__ dbeta) {
+    __shared__ double red[64][17];
     const int col = threadIdx.x & 15, slice = threadIdx.x >> 4, c = blockIdx.x * 16 + col;
     double s = 0.0;
-    if (c < 2 * C)
-        for (int p = slice; p < parts; p += 16) s += (double)part[(long long)p * 2 * C + c];
+    if (c < 2 * C) {
+        int p = slice;
+        for (; p + 192 < parts; p += 256) {
+            float v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = part[(long long)(p + 64 * i) * 2 * C + c];
+            s += (double)v[0] + (double)v[1] + (double)v[2] + (double)v[3];
+        }
+        for (; p < parts; p += 64) s += (double)part[(long long)p * 2 * C + c];
+    }
     red[slice][col] = s;
     __syncthreads();
-    if (slice == 0 && c < 2 * C) {
-        for (int i = 1; i < 16; ++i) s += red[i][col];
-        (c < C ? dgamma[c] : dbeta[c - C]) = (float)s;
+    for (int half = 32; half; half >>= 1) {
+        if (slice < half) red[slice][col] += red[slice + half][col];
+        __syncthreads();
     }
+    if (slice == 0 && c < 2 * C) (c < C ? dgamma[c] : dbeta[c - C]) = (float)red[0][col];
 }
 
 // Lanes of a row (a power of two) and pieces of a lane, at most 4: of the ways that fit, the one with the fewest idle lanes, and of
-// those the one with the most lanes.
+// those the one with the most lanes; more than a wavefront's only where its lanes cannot hold the row.
 struct Rows {
-    int V, L, K;
+    Form form;
+    int L, K;
 };
 bool rows_plan(int C, Rows* p) {
-    if (C <= 0) return false;
-    p->V = C % 8 ? 1 : 8;
-    const int P = C / p->V;
+    if (C <= 0 || C > 16384) return false;
+    p->form = C < 8 ? TINY : C % 8 ? ODD : EVEN;
+    const int P = C < 8 ? C : (C + 7) / 8, most = C < 8 ? 1 : 4;
     p->L = 0;
-    for (int L = 1; L <= 512; L <<= 1) {
+    for (int L = 1; L <= 512; L <<= 1) {      // (512 lanes of 4 pieces: 16384 values)
         const int K = (P + L - 1) / L;
-        if (K <= 4 && (!p->L || L * K <= p->L * p->K)) { p->L = L; p->K = K; }
+        if (K <= most && (!p->L || (L <= 64 && L * K <= p->L * p->K))) { p->L = L; p->K = K; }
     }
-    return p->L != 0;      // up to 2048 pieces
+    return true;
 }
 int threads_of(const Rows& p) { return p.L > 256 ? p.L : 256; }
-constexpr int MOST_PARTS = 1024;
-int parts_of(const Rows& p, size_t rows) {
-    const long long turns = ((long long)rows + threads_of(p) / p.L - 1) / (threads_of(p) / p.L);
-    return (int)(turns < MOST_PARTS ? turns : MOST_PARTS);
+// Workgroups of the backward pass: four for a compute unit, fewer of wide rows, whose registers leave room for two or one and whose sums
+// are a part of the traffic; all with as many turns, but for one (8192 x 4096: 69 us with one, 4096 x 16384: 154 us with four)
+int parts_of(const Rows& p, size_t rows, int C) {
+    const long long most = C <= 1024 ? 1024 : C <= 8192 ? 512 : 256;
+    const long long per = threads_of(p) / p.L, turns = ((long long)rows + per - 1) / per, each = (turns + most - 1) / most;
+    return (int)(each ? (turns + each - 1) / each : 0);
 }
 
 template <typename T>
@@ -198,16 +245,9 @@ int ln_fwd(const void* x, const float* gamma, const float* beta, size_t rows, in
     const long long turns = ((long long)rows + threads / p.L - 1) / (threads / p.L);
     const unsigned grid = (unsigned)(turns < 4096 ? turns : 4096);
     auto go = [&](auto kernel) { kernel<<<grid, threads, 0, (hipStream_t)stream>>>((const T*)x, gamma, beta, (T*)y, (float2*)stats, (long long)rows, C, p.L, eps); };
-    switch (p.V + p.K) {
-        case 2: go(ln_fwd_kernel<T, 1, 1>); break;
-        case 3: go(ln_fwd_kernel<T, 1, 2>); break;
-        case 4: go(ln_fwd_kernel<T, 1, 3>); break;
-        case 5: go(ln_fwd_kernel<T, 1, 4>); break;
-        case 9: go(ln_fwd_kernel<T, 8, 1>); break;
-        case 10: go(ln_fwd_kernel<T, 8, 2>); break;
-        case 11: go(ln_fwd_kernel<T, 8, 3>); break;
-        default: go(ln_fwd_kernel<T, 8, 4>); break;
-    }
+    if (p.form == TINY) go(ln_fwd_kernel<T, TINY, 1>);
+    else if (p.form == EVEN) go(p.K == 1 ? ln_fwd_kernel<T, EVEN, 1> : p.K == 2 ? ln_fwd_kernel<T, EVEN, 2> : p.K == 3 ? ln_fwd_kernel<T, EVEN, 3> : ln_fwd_kernel<T, EVEN, 4>);
+    else go(p.K == 1 ? ln_fwd_kernel<T, ODD, 1> : p.K == 2 ? ln_fwd_kernel<T, ODD, 2> : p.K == 3 ? ln_fwd_kernel<T, ODD, 3> : ln_fwd_kernel<T, ODD, 4>);
     return check_launch();
 }
 
@@ -220,27 +260,20 @@ int ln_bwd(const void* dy, const void* x, const float* stats, const float* gamma
     if (!aligned16(dy) || !aligned16(x) || !aligned16(add) || !aligned16(dx) || !aligned16(ws) || ((uintptr_t)stats & 7)) return MI3D_ERR_INVALID_ARG;
     if (!rows_plan(C, &p) || rows >= (1ull << 40)) return MI3D_ERR_UNSUPPORTED;
     if (ws_bytes < mi3d_layernorm_workspace_bytes(rows, C)) return MI3D_ERR_WORKSPACE;
-    const int threads = threads_of(p), parts = parts_of(p, rows);
+    const int threads = threads_of(p), parts = parts_of(p, rows, C);
     if (parts) {
         auto go = [&](auto kernel) {
             const int per = threads / p.L;
             kernel<<<parts, threads, per > 1 ? (size_t)per * C * sizeof(float) : 0, (hipStream_t)stream>>>(      // (at most 32 KB)
                 (const T*)dy, (const T*)x, (const float2*)stats, gamma, (const T*)add, (T*)dx, (float*)ws, (long long)rows, C, p.L);
         };
-        switch (p.V + p.K) {
-            case 2: go(ln_bwd_kernel<T, 1, 1>); break;
-            case 3: go(ln_bwd_kernel<T, 1, 2>); break;
-            case 4: go(ln_bwd_kernel<T, 1, 3>); break;
-            case 5: go(ln_bwd_kernel<T, 1, 4>); break;
-            case 9: go(ln_bwd_kernel<T, 8, 1>); break;
-            case 10: go(ln_bwd_kernel<T, 8, 2>); break;
-            case 11: go(ln_bwd_kernel<T, 8, 3>); break;
-            default: go(ln_bwd_kernel<T, 8, 4>); break;
-        }
+        if (p.form == TINY) go(ln_bwd_kernel<T, TINY, 1>);
+        else if (p.form == EVEN) go(p.K == 1 ? ln_bwd_kernel<T, EVEN, 1> : p.K == 2 ? ln_bwd_kernel<T, EVEN, 2> : p.K == 3 ? ln_bwd_kernel<T, EVEN, 3> : ln_bwd_kernel<T, EVEN, 4>);
+        else go(p.K == 1 ? ln_bwd_kernel<T, ODD, 1> : p.K == 2 ? ln_bwd_kernel<T, ODD, 2> : p.K == 3 ? ln_bwd_kernel<T, ODD, 3> : ln_bwd_kernel<T, ODD, 4>);
         const int st = check_launch();
         if (st) return st;
     }
-    ln_finish_kernel<<<(2 * C + 15) / 16, 256, 0, (hipStream_t)stream>>>((const float*)ws, parts, C, dgamma, dbeta);
+    ln_finish_kernel<<<(2 * C + 15) / 16, 1024, 0, (hipStream_t)stream>>>((const float*)ws, parts, C, dgamma, dbeta);
     return check_launch();
 }
 
@@ -253,7 +286,7 @@ extern "C" {
 
 size_t mi3d_layernorm_workspace_bytes(size_t rows, int C) {
     Rows p;
-    return rows_plan(C, &p) ? (size_t)parts_of(p, rows) * 2 * C * sizeof(float) : 0;
+    return rows_plan(C, &p) ? (size_t)parts_of(p, rows, C) * 2 * C * sizeof(float) : 0;
 }
 
 int mi3d_layernorm_fwd(const void* x, const float* gamma, const float* beta, size_t rows, int C, float eps, void* y, float* stats, void* stream) {

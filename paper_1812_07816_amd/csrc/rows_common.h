@@ -38,6 +38,26 @@ __device__ __forceinline__ void store_values(T* p, const float (&f)[V]) {
         ((float4*)p)[1] = float4{f[4], f[5], f[6], f[7]};
     }
 }
+// eight values at any address of their type (the memory system takes unaligned pieces)
+template <typename T>
+__device__ __forceinline__ void load8_anywhere(const T* p, float (&f)[8]) {
+    typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)), aligned(2))) uint32_t u32x4;
+    uint4 v[sizeof(T) / 2];
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(T) / 2); ++i) {
+        const u32x4 u = ((const u32x4*)p)[i];
+        v[i] = uint4{u[0], u[1], u[2], u[3]};
+    }
+    load_values<T, 8>((const T*)v, f);
+}
+template <typename T>
+__device__ __forceinline__ void store8_anywhere(T* p, const float (&f)[8]) {
+    typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)), aligned(2))) uint32_t u32x4;
+    uint4 v[sizeof(T) / 2];
+    store_values<T, 8>((T*)v, f);
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(T) / 2); ++i) ((u32x4*)p)[i] = u32x4{v[i].x, v[i].y, v[i].z, v[i].w};
+}
 // the same for 8 values that stay out of the way of what is read again soon
 template <typename T>
 __device__ __forceinline__ void store_streamed(T* p, const float (&f)[8]) {

@@ -12,7 +12,7 @@ HALF = {torch.bfloat16: 2.0 ** -8, torch.float32: 2.0 ** -24}
 DTYPES = [torch.bfloat16, torch.float32]
 # (rows, C): pieces of eight in 1 to 512 lanes, one value at a time, one row, more rows than one turn of the grid takes
 SHAPES = [(1, 8), (1, 1024), (3, 1), (5, 7), (37, 320), (1000, 32), (70001, 8), (513, 24), (129, 1000), (64, 2048), (33, 4096), (9, 4104), (3, 16384),
-          (65, 333), (17, 2047), (40000, 40), (2, 6400), (300, 257), (20, 12288)]
+          (65, 333), (17, 2047), (40000, 40), (2, 6400), (300, 257), (20, 12288), (11, 2051), (5, 16383), (4000, 9), (50, 15), (700, 4095)]
 
 
 def inputs(rows, C, dtype, mean=0.0, seed=0):

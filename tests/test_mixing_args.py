@@ -16,7 +16,7 @@ def test_layernorm_refusals():
         assert f(None, A, A, 4, 8, 1e-5, A, A, None) == INVALID and f(A, A, A, 4, 8, 1e-5, None, A, None) == INVALID
         assert f(A + 2, A, A, 4, 8, 1e-5, A, A, None) == INVALID and f(A, A, A, 4, 8, 1e-5, A, A + 4, None) == INVALID
         assert f(A, A, A, 4, 8, -1.0, A, A, None) == INVALID and f(A, A, A, 4, 8, float("nan"), A, A, None) == INVALID
-        for C in (2049, 16392, 1 << 30):
+        for C in (16385, 16392, 1 << 30):
             assert f(A, A, A, 4, C, 1e-5, A, A, None) == UNSUPPORTED, C
             assert l.mi3d_layernorm_workspace_bytes(4, C) == 0
         assert f(A, A, A, 1 << 40, 8, 1e-5, A, A, None) == UNSUPPORTED
