@@ -32,7 +32,7 @@ def inputs(rows, C, F, O, dtype, seed=0):
 
 def close(got, ref, tol, what=""):
     assert torch.isfinite(got).all(), what
-    off = (got.cpu().double() - ref).abs()
+    off = (got.to(ref.device).double() - ref).abs()
     assert (off <= tol).all(), (what, float((off - tol).max()), float((off / tol).max()))
 
 
@@ -42,11 +42,10 @@ def sums(a, b):
     return a @ b, 2 * U * (k + 1) * (a.abs() @ b.abs()) + 1e-30
 
 
-@pytest.mark.parametrize("dtype", DTYPES, ids=["bf16", "f32"])
-@pytest.mark.parametrize("rows,C,F,O", SHAPES)
-def test_forward(device, rows, C, F, O, dtype):
+def check_forward(device, rows, C, F, O, dtype, where="cpu"):
+    """where: the device that forms the reference."""
     act = "gelu" if F % 16 else "silu"
-    t = inputs(rows, C, F, O, dtype)
+    t = {k: v.to(where) for k, v in inputs(rows, C, F, O, dtype).items()}
     d = ffn.make_desc(rows, C, F, O, act, dtype)
     x, w1, w2 = (t[k].to(device) for k in ("x", "w1", "w2"))
     gu = torch.full((rows, 2 * F), float("nan"), dtype=dtype, device=device)
@@ -70,11 +69,9 @@ def test_forward(device, rows, C, F, O, dtype):
     assert torch.equal(h2, h) and torch.equal(gu2, gu)
 
 
-@pytest.mark.parametrize("dtype", DTYPES, ids=["bf16", "f32"])
-@pytest.mark.parametrize("rows,C,F,O", SHAPES)
-def test_data_gradient(device, rows, C, F, O, dtype):
+def check_data_gradient(device, rows, C, F, O, dtype, where="cpu"):
     act = "silu" if F % 16 else "gelu"
-    t = inputs(rows, C, F, O, dtype)
+    t = {k: v.to(where) for k, v in inputs(rows, C, F, O, dtype).items()}
     d = ffn.make_desc(rows, C, F, O, act, dtype)
     dx, dgu, h = ffn.ffn_dgrad(d, *(t[k].to(device) for k in ("dy", "w1", "w2", "gu")))
     g, u = t["gu"][:, :F].double(), t["gu"][:, F:].double()
@@ -93,10 +90,8 @@ def test_data_gradient(device, rows, C, F, O, dtype):
     close(dx, rx, 1.01 * (HALF[dtype] * rx.abs() + ex), "dx")
 
 
-@pytest.mark.parametrize("dtype", DTYPES, ids=["bf16", "f32"])
-@pytest.mark.parametrize("rows,C,F,O", SHAPES + [(0, 16, 24, 8), (9000, 64, 72, 40)])
-def test_weight_gradient(device, rows, C, F, O, dtype):
-    t = inputs(rows, C, F, O, dtype)
+def check_weight_gradient(device, rows, C, F, O, dtype, where="cpu"):
+    t = {k: v.to(where) for k, v in inputs(rows, C, F, O, dtype).items()}
     d = ffn.make_desc(rows, C, F, O, "silu", dtype)
     args = [t[k].to(device) for k in ("x", "dgu", "h", "dy")]
     dw1, dw2 = ffn.ffn_wgrad(d, *args, dw1=torch.full((2 * F, C), float("nan"), device=device), dw2=torch.full((O, F), float("nan"), device=device))
@@ -104,6 +99,55 @@ def test_weight_gradient(device, rows, C, F, O, dtype):
     close(dw2, *sums(t["dy"].double().t(), t["h"].double()), "dw2")
     again = ffn.ffn_wgrad(d, *args)
     assert torch.equal(again[0], dw1) and torch.equal(again[1], dw2)
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=["bf16", "f32"])
+@pytest.mark.parametrize("rows,C,F,O", SHAPES)
+def test_forward(device, rows, C, F, O, dtype):
+    check_forward(device, rows, C, F, O, dtype)
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=["bf16", "f32"])
+@pytest.mark.parametrize("rows,C,F,O", SHAPES)
+def test_data_gradient(device, rows, C, F, O, dtype):
+    check_data_gradient(device, rows, C, F, O, dtype)
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=["bf16", "f32"])
+@pytest.mark.parametrize("rows,C,F,O", SHAPES + [(0, 16, 24, 8), (9000, 64, 72, 40)])
+def test_weight_gradient(device, rows, C, F, O, dtype):
+    check_weight_gradient(device, rows, C, F, O, dtype)
+
+
+L, M, S, FEW = "tiles_256x256", "tiles_128x128", "tiles_64x128", "few_rows"
+# a shape for each kernel of a product, with its contraction whole and in parts (0: any number of parts above one)
+EACH = [("fwd", "bf16", (17612, 272, 352, 8), L, None), ("fwd", "bf16", (583, 8, 3656, 8), M, None), ("fwd", "bf16", (1132, 8, 160, 8), S, None),
+        ("fwd", "bf16", (7536, 24, 280, 1776), None, (L, 1)), ("fwd", "bf16", (18684, 16, 2680, 144), None, (L, 0)), ("fwd", "bf16", (17204, 16, 8, 184), None, (M, 1)),
+        ("fwd", "bf16", (9036, 16, 3088, 24), None, (M, 0)), ("fwd", "bf16", (40, 40, 8, 3160), None, (S, 1)), ("fwd", "bf16", (41, 104, 1544, 2728), None, (S, 0)),
+        ("fwd", "bf16", (300, 200, 520, 200), FEW, (FEW, 1)),
+        ("fwd", "f32", (799, 8, 2592, 8), M, None), ("fwd", "f32", (3159, 8, 24, 8), S, None), ("fwd", "f32", (300, 200, 520, 200), FEW, (FEW, 1)),
+        ("fwd", "f32", (11640, 8, 8, 264), None, (M, 1)), ("fwd", "f32", (8470, 8, 936, 40), None, (M, 0)), ("fwd", "f32", (19, 120, 8, 3200), None, (S, 1)),
+        ("fwd", "f32", (1, 8, 3552, 8), None, (S, 0)),
+        ("dgrad", "bf16", (3725, 8, 3448, 736), L, None), ("dgrad", "bf16", (19587, 8, 136, 8), M, None), ("dgrad", "bf16", (3224, 3944, 136, 16), None, (L, 1)),
+        ("dgrad", "bf16", (16702, 152, 1200, 32), None, (L, 0)), ("dgrad", "bf16", (16506, 160, 8, 16), None, (M, 1)), ("dgrad", "bf16", (10804, 8, 1200, 8), None, (M, 0)),
+        ("dgrad", "bf16", (2, 8, 552, 8), S, (S, 0)), ("dgrad", "f32", (12818, 8, 296, 8), M, None), ("dgrad", "f32", (19045, 152, 8, 56), None, (M, 1)),
+        ("dgrad", "f32", (4790, 8, 800, 8), None, (M, 0)),
+        ("wgrad", "bf16", (272, 1512, 2528, 1808), None, ("pair " + L, 1)), ("wgrad", "bf16", (4645, 136, 3752, 144), None, ("pair " + L, 0)),
+        ("wgrad", "bf16", (1, 440, 3968, 8), None, ("pair " + M, 1)), ("wgrad", "bf16", (14361, 8, 8, 1136), None, ("pair " + M, 0)),
+        ("wgrad", "bf16", (1120, 8, 8, 8), None, ("pair " + S, 0)), ("wgrad", "bf16", (15379, 176, 3816, 8), L, (S, 0)), ("wgrad", "bf16", (331, 152, 2344, 3008), S, (M, 1)),
+        ("wgrad", "f32", (2552, 24, 8, 3232), None, ("pair " + M, 0)), ("wgrad", "f32", (435, 8, 8, 16), None, ("pair " + S, 0)),
+        ("wgrad", "f32", (4455, 8, 4096, 8), M, (S, 0)), ("wgrad", "f32", (386, 16, 1992, 1856), S, (S, 1))]
+
+
+@pytest.mark.parametrize("way,dt,shape,first,second", EACH)
+def test_each_kernel_with_whole_and_split_contractions(device, way, dt, shape, first, second):
+    dtype = {"bf16": torch.bfloat16, "f32": torch.float32}[dt]
+    how = ffn.kernel_detail(ffn.make_desc(*shape, "silu", dtype), ("fwd", "dgrad", "wgrad").index(way)).split(", ")
+    assert first is None or how[0].split(" parts")[0] == first, how
+    if second is not None:
+        name, parts = how[-1].split(" parts ")
+        assert name == second[0] and (int(parts) > 1 if second[1] == 0 else int(parts) == second[1]), how
+    {"fwd": check_forward, "dgrad": check_data_gradient, "wgrad": check_weight_gradient}[way](device, *shape, dtype, where=device)
 
 
 @pytest.mark.parametrize("dtype", DTYPES, ids=["bf16", "f32"])

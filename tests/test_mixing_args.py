@@ -69,6 +69,40 @@ def test_ffn_refusals():
     assert l.mi3d_ffn_fwd(none, None, A, A, None, None, None, 0, None) == 0 and l.mi3d_ffn_dgrad(none, None, A, A, None, None, None, None, None, 0, None) == 0
 
 
+def test_kernel_detail_says_what_runs_and_refuses_what_a_call_refuses():
+    l, buf = _lib.lib(), ctypes.create_string_buffer(64)
+    d = ffn.make_desc(1, 1024, 4096, 1024, "silu", torch.bfloat16)
+    assert ffn.kernel_detail(d, ffn.PASS_FWD) == "few_rows, few_rows parts 1"
+    d = ffn.make_desc(16384, 1024, 4096, 1024, "gelu", torch.bfloat16)
+    assert ffn.kernel_detail(d, ffn.PASS_DGRAD) == "tiles_256x256, tiles_256x256 parts 1" and ffn.workspace_bytes(d, ffn.PASS_DGRAD) == 0
+    assert l.mi3d_ffn_kernel_detail(ctypes.byref(d), 3, buf, 64) == INVALID and l.mi3d_ffn_kernel_detail(ctypes.byref(d), 0, None, 64) == INVALID
+    d.Cin = 12
+    assert l.mi3d_ffn_kernel_detail(ctypes.byref(d), 0, buf, 64) == UNSUPPORTED
+
+
+def test_plans_do_not_depend_on_what_was_asked_before():
+    """A thread keeps its last plans: the same answers in any order and in other threads."""
+    import random
+    import threading
+    r = random.Random(5)
+    asks = [(ffn.make_desc(r.randint(1, 9000), 8 * r.randint(1, 200), 8 * r.randint(1, 400), 8 * r.randint(1, 200), "silu", r.choice([torch.bfloat16, torch.float32])), q)
+            for _ in range(120) for q in range(3)]
+    said = [(ffn.kernel_detail(*a), ffn.workspace_bytes(*a)) for a in asks]
+    wrong = []
+
+    def again(order):
+        wrong.extend(i for i in order if (ffn.kernel_detail(*asks[i]), ffn.workspace_bytes(*asks[i])) != said[i])
+
+    order = list(range(len(asks)))
+    r.shuffle(order)
+    threads = [threading.Thread(target=again, args=(o,)) for o in (order, order[::-1])]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong
+
+
 def test_the_binding_refuses_before_the_library_is_called():
     """Tensors on the host, of another type or shape, or not dense."""
     x, g = torch.zeros(4, 8), torch.zeros(8)
