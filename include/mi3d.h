@@ -2,7 +2,7 @@
  * mi3d — C ABI of the MI355X (gfx950) hot path for full-resolution 3D U-Net
  * training with data swapping.
  *
- * Two groups of entry points:
+ * Groups of entry points:
  *   1. mi3d_conv3d_{fwd,dgrad,wgrad}: the 3-D convolution layers whose
  *      forward output ("feature map A^l") is produced in the forward pass and
  *      needed again by the same layer in the backward pass (paper, Section
@@ -13,6 +13,9 @@
  *      are copied to host memory after the forward pass has used them and
  *      copied back before the layer's backward pass, on side streams so that
  *      the copies overlap GPU computation.
+ *   3. The steps around the convolutions, and the parts of a residual
+ *      channel-mixing block (layer normalisation, gated feed-forward block,
+ *      dropout).
  *
  * General rules
  *   - Plain C, no C++ or framework types.  `stream` arguments are a

@@ -5,10 +5,18 @@
 //
 // Every product is one kernel, D[m][n] = sum_k Q(m, k) P(n, k), whose operands lie in memory with k running along rows (x, w1, h,
 // w2 in the forward pass) or across them (w2, w1 in the data gradient, everything in the weight gradient).  Each is fetched as it
-// lies, by loads that go to LDS directly, 128 bytes of k a step: operands with k across are read from there transposed
+// lies, by loads that go to LDS directly, 64 or 128 bytes of k a step: operands with k across are read from there transposed
 // (bf16: ds_read_b64_tr_b16), so that no pass rewrites a tensor or the weights.  P goes into the first operand of the matrix
 // instruction, whose results a lane then holds as four neighbouring n of one row.  bf16: v_mfma_f32_32x32x16_bf16; fp32:
-// v_mfma_f32_32x32x2_f32 on the same 16-byte pieces, four of k.  Sums in fp32.  Bound: the matrix instructions.
+// v_mfma_f32_32x32x2_f32 on the same 16-byte pieces, four of k.  Sums in fp32.  Tensors between two calls are rounded to their type
+// once (h, [dg | du]), as the convolutions' are.
+//
+// Bound: the matrix instructions on long contractions (8192 x 4096 x 8192: 1358 TFLOP/s, where a library product of 8192^3 reaches
+// 1275; fp32 131, and 130); the results of short ones, which every workgroup has to write (and for the data gradient read [g | u])
+// before its compute unit goes on: 16384 x 1024 x 4096 data gradient 237 + 231 us, 27648 x 320 x 1280 forward 82 + 45 us.
+// Measured on the way (16384 x 1024 x 4096, data gradient): results straight from registers, 8 bytes a lane, 811 us; through LDS 571;
+// without bank conflicts the same; fragments a turn ahead and loads between the products 475; results streamed 443 to 470
+// (by device).  Not faster: two to four workgroups of smaller tiles on a unit, deeper rings, workgroups of a unit out of step, wave priorities.
 
 #include <cstdio>
 
@@ -97,7 +105,7 @@ struct Operand {
 };
 
 // A workgroup of WM x WN waves owns 32 MB WM rows x 64 WN columns of D (GATE: columns of g and of u, half each); a wave MB x 2 blocks of
-// 32 x 32.  A step is KB bytes of k; RING steps have a place in LDS, RING - 1 are under way while one is computed.
+// 32 x 32.  A step is KB bytes of k; RING steps have a place in LDS, of which RING - 1 come in while one is computed.
 template <typename T, int MB, int WM, int WN, int KB, int RING, bool QA, bool PA, Form FORM, int ACT>
 __device__ __forceinline__ void ffn_tile(const FfnParams& P, const int block) {
     constexpr int W = WM * WN, BM = 32 * MB * WM, BN = 64 * WN, E = sizeof(T), KS = KB / E;
@@ -189,7 +197,7 @@ __device__ __forceinline__ void ffn_tile(const FfnParams& P, const int block) {
     // A step is KK turns of sixteen (fp32: eight) k.  Between a turn's products stand the reads of the next turn's fragments and a
     // share of a step's loads, so that no wave stands in line for LDS or the address unit while its matrix unit idles; before the last
     // turn's stands the barrier behind which the next step is read and this step's place filled.
-    constexpr int KK = KB / 32, NR = MB + 2, NM = 2 * MB;
+    constexpr int KK = KB / 32, NR = MB + 2, NM = 2 * MB, TP = 2;      // TP: turns that share a step's loads (1 and 4: up to 7 % slower)
     typename OQ::Frag vq[2][MB];
     typename OP::Frag vp[2][2];
     auto read = [&](const char* l, int kk, int to, int j) {      // in the order of the products
@@ -202,9 +210,9 @@ __device__ __forceinline__ void ffn_tile(const FfnParams& P, const int block) {
             begin(s0 + i);
 #pragma unroll
             for (int j = 0; j < NL; ++j)
-                if (i < RING - 1 || j < NL / KK) load(j);      // (the rest of the last one in the first step's turns)
+                if (i < RING - 1 || j < NL / TP) load(j);      // (the rest of the last one in the first step's turns)
         }
-        asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((RING - 2) * NL + NL / KK) : "memory");
+        asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((RING - 2) * NL + NL / TP) : "memory");
 #pragma unroll
         for (int j = 0; j < NR; ++j) read(lds, 0, 0, j);
     }
@@ -235,9 +243,12 @@ __device__ __forceinline__ void ffn_tile(const FfnParams& P, const int block) {
                 for (int j = 0; j < NR; ++j)
                     if (j * NM / NR == m) read(l, kk < KK - 1 ? kk + 1 : 0, (kk + 1) & 1, j);
                 const int part = kk == KK - 1 ? 0 : kk + 1;      // of the step's loads
+                if (part < TP) {
+                    const int j0 = NL * part / TP, j1 = NL * (part + 1) / TP;
 #pragma unroll
-                for (int j = NL * part / KK; j < NL * (part + 1) / KK; ++j)
-                    if ((j - NL * part / KK) * NM / (NL * (part + 1) / KK - NL * part / KK) == m) load(j);
+                    for (int j = j0; j < j1; ++j)
+                        if ((j - j0) * NM / (j1 - j0) == m) load(j);
+                }
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
@@ -422,11 +433,12 @@ int launch_pair(FfnPair P, hipStream_t s) {
 //
 // The time of a product on tiles is rounds of workgroups (one or two on a compute unit), each of which takes a fixed time (first
 // loads, results) and a time for every 128 bytes of k; less where it has its compute unit for itself.  Microseconds, measured over
-// 300 to 27648 rows, 200 to 4096 channels and F 520 to 8192 (the design doc has the table):
-//   LARGE  256 x 256, 8 waves: 1.36 PFLOP/s on long contractions, where LDS reads per product are fewest, but alone on its unit
-//   MIDDLE 128 x 128: two on a unit, which cover each other's first loads and results; best for short contractions
-//   SMALL  64 x 128: fills the chip with a quarter of the rows
-//   FEW    no LDS (ffn_few.hip): small matrices and few rows
+// 300 to 27648 rows, 200 to 4096 channels and F 520 to 8192 (LARGE, MIDDLE, SMALL in us):
+//   LARGE  256 x 256, 8 waves: fewest LDS reads a product, but alone on its unit: dx of 16384 x 1024 x 4096 231, 297, 377
+//   MIDDLE 128 x 128: two on a unit, which cover some of each other's first loads and results, for short contractions:
+//          first product of 27648 x 320 x 1280 90, 82, 115
+//   SMALL  64 x 128: fills the chip with a quarter of the rows: second product of 3456 x 320 x 1280 30, 19, 11
+//   FEW    no LDS (ffn_few.hip): small matrices and few rows: first product of 300 x 200 x 520 SMALL 6.5, FEW 4.2
 enum Tile { LARGE, MIDDLE, SMALL, FEW };
 struct TileTimes {
     int bm, bn, per_cu;
