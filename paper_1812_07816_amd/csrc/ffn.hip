@@ -12,11 +12,11 @@
 // once (h, [dg | du]), as the convolutions' are.
 //
 // Bound: the matrix instructions on long contractions (8192 x 4096 x 8192: 1358 TFLOP/s, where a library product of 8192^3 reaches
-// 1275; fp32 131, and 130); the results of short ones, which every workgroup has to write (and for the data gradient read [g | u])
-// before its compute unit goes on: 16384 x 1024 x 4096 data gradient 237 + 231 us, 27648 x 320 x 1280 forward 82 + 45 us.
+// 1275; fp32, 16384 x 1024 x 4096, 132 to 139, and 130); the results of short ones, which every workgroup has to write (and for the data gradient read [g | u])
+// before its compute unit goes on: 16384 x 1024 x 4096 data gradient 247 + 228 us, 27648 x 320 x 1280 forward 87 + 41 us.
 // Measured on the way (16384 x 1024 x 4096, data gradient): results straight from registers, 8 bytes a lane, 811 us; through LDS 571;
-// without bank conflicts the same; fragments a turn ahead and loads between the products 475; results streamed 443 to 470
-// (by device).  Not faster: two to four workgroups of smaller tiles on a unit, deeper rings, workgroups of a unit out of step, wave priorities.
+// without bank conflicts the same; fragments a turn ahead and loads between the products 475; results streamed 443 to 475
+// (by device; the two kernels alone).  Not faster: two to four workgroups of smaller tiles on a unit, deeper rings, workgroups of a unit out of step, wave priorities.
 
 #include <cstdio>
 

@@ -3,7 +3,8 @@
 // Backward, from x and the row's (mean, rstd), with g = dy * gamma:
 //   dx = rstd * (g - mean_c(g) - xhat * mean_c(g * xhat)) (+ add),  dgamma = sum_rows dy * xhat,  dbeta = sum_rows dy.
 //
-// Bound: HBM (bf16, 192^3 rows of 32: forward 185 us, backward with a second gradient 345 us = 5.25 TB/s, where a copy reaches 5.15; 27648
+// Bound: HBM (bf16, 192^3 rows of 32: forward 185 us, backward with a second gradient 345 us = 5.25 TB/s of
+// the tensors alone, 5.4 with the rows' statistics, where a copy reaches 5.15; 27648
 // rows of 320: 10 and 23 us).  A row stays in the registers of L lanes, K pieces of eight values each, so that it is read once and the
 // variance is a sum of squared differences from the mean (no cancellation where the mean is large); sums in fp32.  The
 // sums over rows are kept per lane (a lane always has the same channels), added over the lanes of a workgroup in lane
