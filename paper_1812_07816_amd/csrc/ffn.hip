@@ -379,12 +379,13 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) ffn_outer_pair_kernel(const F
 long long tiles_of(long long n, int tile) { return (n + tile - 1) / tile; }
 
 // what the kernel needs to find its tile; false: too many
-bool number_tiles(FfnParams* P, int bm, int cols, int bn, int ks) {
+// (a launch counts its threads in 32 bits)
+bool number_tiles(FfnParams* P, int bm, int cols, int bn, int ks, int threads) {
     P->mt = (int)tiles_of(P->M, bm);
     P->nt = (int)tiles_of(cols, bn);
     const long long tiles = (long long)P->mt * P->nt, steps = tiles_of(P->K, ks);
     if (P->splits < 1) P->splits = 1;
-    if (tiles * P->splits >= (1ll << 30) || steps >= (1ll << 31)) return false;
+    if (tiles * P->splits * threads >= (1ll << 31) || steps >= (1ll << 31)) return false;
     P->per = (int)(steps / P->splits);
     P->extra = (int)(steps % P->splits);
     P->tiles = make_div((uint32_t)tiles);
@@ -402,7 +403,7 @@ int allow_lds(Kernel kernel, int bytes) {
 template <typename T, int MB, int WM, int WN, int KB, int RING, bool QA, bool PA, Form FORM, int ACT>
 int launch(FfnParams P, hipStream_t s) {
     constexpr int BM = 32 * MB * WM, BN = 64 * WN, LDS = RING * (BM + BN) * KB;
-    if (!number_tiles(&P, BM, FORM == GATE ? P.F : P.N, FORM == GATE ? BN / 2 : BN, KB / sizeof(T))) return MI3D_ERR_UNSUPPORTED;
+    if (!number_tiles(&P, BM, FORM == GATE ? P.F : P.N, FORM == GATE ? BN / 2 : BN, KB / sizeof(T), 64 * WM * WN)) return MI3D_ERR_UNSUPPORTED;
     const auto kernel = ffn_gemm_kernel<T, MB, WM, WN, KB, RING, QA, PA, FORM, ACT>;
     static std::atomic<bool> attr_set{false};   // set once per process; a second thread racing here repeats an idempotent call
     if (!attr_set) {
@@ -416,7 +417,7 @@ int launch(FfnParams P, hipStream_t s) {
 template <typename T, int MB, int WM, int WN, int KB, int RING>
 int launch_pair(FfnPair P, hipStream_t s) {
     constexpr int BM = 32 * MB * WM, BN = 64 * WN, LDS = RING * (BM + BN) * KB;
-    if (!number_tiles(&P.a, BM, P.a.N, BN, KB / sizeof(T)) || !number_tiles(&P.b, BM, P.b.N, BN, KB / sizeof(T))) return MI3D_ERR_UNSUPPORTED;
+    if (!number_tiles(&P.a, BM, P.a.N, BN, KB / sizeof(T), 64 * WM * WN) || !number_tiles(&P.b, BM, P.b.N, BN, KB / sizeof(T), 64 * WM * WN)) return MI3D_ERR_UNSUPPORTED;
     P.first = (int)(P.a.tiles.d * P.a.splits + 7) / 8 * 8;
     const auto kernel = ffn_outer_pair_kernel<T, MB, WM, WN, KB, RING>;
     static std::atomic<bool> attr_set{false};

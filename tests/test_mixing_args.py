@@ -69,6 +69,14 @@ def test_ffn_refusals():
     assert l.mi3d_ffn_fwd(none, None, A, A, None, None, None, 0, None) == 0 and l.mi3d_ffn_dgrad(none, None, A, A, None, None, None, None, None, 0, None) == 0
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_ffn_refuses_more_workgroups_than_a_launch_holds(dtype):
+    """2^31 - 1 rows of eight channels are 2^24 tiles of 256 threads: 2^32, one more than a launch counts."""
+    l, r = _lib.lib(), ctypes.byref(ffn.make_desc(2 ** 31 - 1, 8, 8, 8, "silu", dtype))
+    assert l.mi3d_ffn_gate(r, A, A, A, None, None) == UNSUPPORTED and l.mi3d_ffn_fwd(r, A, A, A, A, None, A, 1 << 40, None) == UNSUPPORTED
+    assert l.mi3d_ffn_dgrad(r, A, A, A, A, A, A, A, A, 1 << 40, None) == UNSUPPORTED
+
+
 def test_kernel_detail_says_what_runs_and_refuses_what_a_call_refuses():
     l, buf = _lib.lib(), ctypes.create_string_buffer(64)
     d = ffn.make_desc(1, 1024, 4096, 1024, "silu", torch.bfloat16)
