@@ -393,11 +393,20 @@ bool number_tiles(FfnParams* P, int bm, int cols, int bn, int ks, int threads) {
     P->last = make_div(P->mt % 4 ? P->mt % 4 : 4);
     return true;
 }
+// Once for each device (bits of `done`), as the attribute belongs to the current one; a second thread racing here repeats an idempotent call
 template <class Kernel>
-int allow_lds(Kernel kernel, int bytes) {
-    const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (e != hipSuccess) note_hip_error(e);
-    return e == hipSuccess ? MI3D_OK : MI3D_ERR_HIP;
+int allow_lds(Kernel kernel, int bytes, std::atomic<uint64_t>& done) {
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    const uint64_t bit = 1ull << (dev & 63);
+    if (e == hipSuccess && dev < 64 && done & bit) return MI3D_OK;
+    if (e == hipSuccess) e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != hipSuccess) {
+        note_hip_error(e);
+        return MI3D_ERR_HIP;
+    }
+    if (dev < 64) done |= bit;
+    return MI3D_OK;
 }
 
 template <typename T, int MB, int WM, int WN, int KB, int RING, bool QA, bool PA, Form FORM, int ACT>
@@ -405,12 +414,9 @@ int launch(FfnParams P, hipStream_t s) {
     constexpr int BM = 32 * MB * WM, BN = 64 * WN, LDS = RING * (BM + BN) * KB;
     if (!number_tiles(&P, BM, FORM == GATE ? P.F : P.N, FORM == GATE ? BN / 2 : BN, KB / sizeof(T), 64 * WM * WN)) return MI3D_ERR_UNSUPPORTED;
     const auto kernel = ffn_gemm_kernel<T, MB, WM, WN, KB, RING, QA, PA, FORM, ACT>;
-    static std::atomic<bool> attr_set{false};   // set once per process; a second thread racing here repeats an idempotent call
-    if (!attr_set) {
-        const int st = allow_lds(kernel, LDS);
-        if (st) return st;
-        attr_set = true;
-    }
+    static std::atomic<uint64_t> allowed{0};
+    const int st = allow_lds(kernel, LDS, allowed);
+    if (st) return st;
     kernel<<<P.tiles.d * P.splits, 64 * WM * WN, LDS, s>>>(P);
     return check_launch();
 }
@@ -420,12 +426,9 @@ int launch_pair(FfnPair P, hipStream_t s) {
     if (!number_tiles(&P.a, BM, P.a.N, BN, KB / sizeof(T), 64 * WM * WN) || !number_tiles(&P.b, BM, P.b.N, BN, KB / sizeof(T), 64 * WM * WN)) return MI3D_ERR_UNSUPPORTED;
     P.first = (int)(P.a.tiles.d * P.a.splits + 7) / 8 * 8;
     const auto kernel = ffn_outer_pair_kernel<T, MB, WM, WN, KB, RING>;
-    static std::atomic<bool> attr_set{false};
-    if (!attr_set) {
-        const int st = allow_lds(kernel, LDS);
-        if (st) return st;
-        attr_set = true;
-    }
+    static std::atomic<uint64_t> allowed{0};
+    const int st = allow_lds(kernel, LDS, allowed);
+    if (st) return st;
     kernel<<<P.first + P.b.tiles.d * P.b.splits, 64 * WM * WN, LDS, s>>>(P);
     return check_launch();
 }
