@@ -396,8 +396,9 @@ int mi3d_dropout_channels_f32(const float *a, float *out, int N, size_t voxels, 
  *   [g | u] = x w1^T,   h = act(g) * u,   y = h w2^T
  * x [rows][Cin], w1 [2 F][Cin] (the gate's F rows first), gu [rows][2 F], h [rows][F], w2 [Cout][F], y [rows][Cout], all of
  * the descriptor's type.  act: MI3D_ACT_SILU, a / (1 + e^-a), or MI3D_ACT_GELU, a Phi(a) with the normal distribution's Phi.
- * Cin, F and Cout in multiples of 8 up to 65536, rows < 2^31, and a product of no more tiles than a launch of 2^31 threads has
- * (8 channels: some 2^30 rows are too many); others return MI3D_ERR_UNSUPPORTED.  Tensors of one call must not overlap.  ws: mi3d_ffn_workspace_bytes(desc, MI3D_PASS_*) bytes, else MI3D_ERR_WORKSPACE. */
+ * Cin, F and Cout in multiples of 8 up to 65536, rows < 2^31, and each product of no more tiles than a launch of 2^31 threads has
+ * (8 channels: some 2^30 rows are too many); others return MI3D_ERR_UNSUPPORTED from every call, before anything is launched (mi3d_ffn_gate, which
+ * forms no y, asks for its own product only).  Tensors of one call must not overlap.  ws: mi3d_ffn_workspace_bytes(desc, MI3D_PASS_*) bytes, else MI3D_ERR_WORKSPACE. */
 typedef enum { MI3D_ACT_SILU = 0, MI3D_ACT_GELU = 1 } mi3d_act;
 typedef struct {
     long long rows;

@@ -378,20 +378,17 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) ffn_outer_pair_kernel(const F
 
 long long tiles_of(long long n, int tile) { return (n + tile - 1) / tile; }
 
-// what the kernel needs to find its tile; false: too many
-// (a launch counts its threads in 32 bits)
-bool number_tiles(FfnParams* P, int bm, int cols, int bn, int ks, int threads) {
+// what the kernel needs to find its tile (the plan has seen to it that a launch holds them)
+void number_tiles(FfnParams* P, int bm, int cols, int bn, int ks) {
     P->mt = (int)tiles_of(P->M, bm);
     P->nt = (int)tiles_of(cols, bn);
     const long long tiles = (long long)P->mt * P->nt, steps = tiles_of(P->K, ks);
     if (P->splits < 1) P->splits = 1;
-    if (tiles * P->splits * threads >= (1ll << 31) || steps >= (1ll << 31)) return false;
     P->per = (int)(steps / P->splits);
     P->extra = (int)(steps % P->splits);
     P->tiles = make_div((uint32_t)tiles);
     P->band = make_div(4u * P->nt);
     P->last = make_div(P->mt % 4 ? P->mt % 4 : 4);
-    return true;
 }
 // Once for each device (bits of `done`), as the attribute belongs to the current one; a second thread racing here repeats an idempotent call
 template <class Kernel>
@@ -412,7 +409,7 @@ int allow_lds(Kernel kernel, int bytes, std::atomic<uint64_t>& done) {
 template <typename T, int MB, int WM, int WN, int KB, int RING, bool QA, bool PA, Form FORM, int ACT>
 int launch(FfnParams P, hipStream_t s) {
     constexpr int BM = 32 * MB * WM, BN = 64 * WN, LDS = RING * (BM + BN) * KB;
-    if (!number_tiles(&P, BM, FORM == GATE ? P.F : P.N, FORM == GATE ? BN / 2 : BN, KB / sizeof(T), 64 * WM * WN)) return MI3D_ERR_UNSUPPORTED;
+    number_tiles(&P, BM, FORM == GATE ? P.F : P.N, FORM == GATE ? BN / 2 : BN, KB / sizeof(T));
     const auto kernel = ffn_gemm_kernel<T, MB, WM, WN, KB, RING, QA, PA, FORM, ACT>;
     static std::atomic<uint64_t> allowed{0};
     const int st = allow_lds(kernel, LDS, allowed);
@@ -423,7 +420,8 @@ int launch(FfnParams P, hipStream_t s) {
 template <typename T, int MB, int WM, int WN, int KB, int RING>
 int launch_pair(FfnPair P, hipStream_t s) {
     constexpr int BM = 32 * MB * WM, BN = 64 * WN, LDS = RING * (BM + BN) * KB;
-    if (!number_tiles(&P.a, BM, P.a.N, BN, KB / sizeof(T), 64 * WM * WN) || !number_tiles(&P.b, BM, P.b.N, BN, KB / sizeof(T), 64 * WM * WN)) return MI3D_ERR_UNSUPPORTED;
+    number_tiles(&P.a, BM, P.a.N, BN, KB / sizeof(T));
+    number_tiles(&P.b, BM, P.b.N, BN, KB / sizeof(T));
     P.first = (int)(P.a.tiles.d * P.a.splits + 7) / 8 * 8;
     const auto kernel = ffn_outer_pair_kernel<T, MB, WM, WN, KB, RING>;
     static std::atomic<uint64_t> allowed{0};
@@ -445,17 +443,26 @@ int launch_pair(FfnPair P, hipStream_t s) {
 //   FEW    no LDS (ffn_few.hip): small matrices and few rows: first product of 300 x 200 x 520 SMALL 6.5, FEW 4.2
 enum Tile { LARGE, MIDDLE, SMALL, FEW };
 struct TileTimes {
-    int bm, bn, per_cu;
+    int bm, bn, threads, per_cu;
     double fixed, dact, alone, shared;      // per round, the same for the data gradient's first product; per 128 bytes of k
 };
-constexpr TileTimes TIMES_BF16[3] = {{256, 256, 1, 12.0, 34.0, 1.6, 1.6}, {128, 128, 2, 4.8, 14.0, 0.70, 1.09}, {64, 128, 2, 3.7, 8.6, 0.38, 0.68}};
-constexpr TileTimes TIMES_F32[3] = {{256, 256, 1, 12.0, 34.0, 7.8, 7.8}, {128, 128, 2, 4.8, 14.0, 2.2, 3.7}, {64, 128, 2, 3.7, 8.6, 1.2, 2.1}};
+constexpr TileTimes TIMES_BF16[3] = {{256, 256, 512, 1, 12.0, 34.0, 1.6, 1.6}, {128, 128, 256, 2, 4.8, 14.0, 0.70, 1.09}, {64, 128, 256, 2, 3.7, 8.6, 0.38, 0.68}};
+constexpr TileTimes TIMES_F32[3] = {{256, 256, 512, 1, 12.0, 34.0, 7.8, 7.8}, {128, 128, 256, 2, 4.8, 14.0, 2.2, 3.7}, {64, 128, 256, 2, 3.7, 8.6, 1.2, 2.1}};
 
 struct Plan {
     Tile tile;
     int splits;
     double us;
+    bool fits() const { return us < 1e30; }      // false: no tiles of which a launch holds as many as it takes
 };
+// (a launch counts its threads in 32 bits)
+constexpr long long MOST_THREADS = (1ll << 31) - 1;
+// Slices of the parts that ffn_add_parts_kernel's threads take side by side
+int slices_of(int parts) {
+    int S = 1;
+    while (S < 8 && 2 * S <= parts) S *= 2;
+    return S;
+}
 double tiles_us(const TileTimes& t, bool dact, long long tiles, double steps) {
     const long long cus = cu_count(), slots = t.per_cu * cus, rest = tiles % slots;
     const double fixed = dact ? t.dact : t.fixed;
@@ -471,8 +478,11 @@ Plan plan(Form form, int e, long long M, long long cols, long long K, int most_p
     for (int i = e == 2 ? 0 : 1; i < 3; ++i) {      // (fp32: LARGE has nothing to save, the matrix instructions take eight times longer)
         const TileTimes& t = (e == 2 ? TIMES_BF16 : TIMES_F32)[i];
         const long long tiles = tiles_of(M, t.bm) * tiles_of(cols, t.bn) + tiles_of(M2, t.bm) * tiles_of(cols2, t.bn);
+        const long long n = M * cols + M2 * cols2;
         for (int s = 1; s <= most_parts && (s == 1 || s * 4 <= steps); s += s < 8 ? 1 : s / 4) {
-            const double us = tiles_us(t, form == DACT, tiles * s, steps / s) + add_us(s, (double)M * cols + (double)M2 * cols2);
+            // (up to 7 workgroups between two products, one more in each addition)
+            if ((tiles * s + 7) * t.threads > MOST_THREADS || (s > 1 && (n / 8 * slices_of(s) + 512) > MOST_THREADS)) continue;
+            const double us = tiles_us(t, form == DACT, tiles * s, steps / s) + add_us(s, (double)n);
             if (us < best.us) best = Plan{(Tile)i, s, us};
         }
     }
@@ -537,8 +547,7 @@ __global__ void __launch_bounds__(256) ffn_add_parts_kernel(const Parts<T> a, co
 }
 template <typename T>
 int add_parts(const float* part, T* out, long long n, const float* part2, T* out2, long long n2, int parts, hipStream_t s) {
-    int S = 1;
-    while (S < 8 && 2 * S <= parts) S *= 2;
+    const int S = slices_of(parts);
     const int values = 256 / S * 8;
     const Parts<T> a = {part, out, n, (int)tiles_of(n, values)}, b = {part2, out2, n2, (int)tiles_of(n2, values)};
     ffn_add_parts_kernel<T><<<(unsigned)(a.blocks + b.blocks), 256, 0, s>>>(a, b, parts, S);
@@ -564,6 +573,7 @@ size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 struct Plans {
     Plan first, second;
     bool pair;
+    bool fit() const { return first.fits() && second.fits(); }
 };
 Plans make_plans(const Desc& d, int pass) {
     if (pass == MI3D_PASS_FWD) return Plans{plan(GATE, d.e, d.rows, 2 * d.F, d.C, 1), plan(STORE, d.e, d.rows, d.O, d.F, MOST_PARTS), false};
@@ -594,10 +604,11 @@ size_t parts_bytes(int splits, long long M, long long N) { return splits > 1 ? (
 bool usable(const void* p) { return p && aligned16(p); }
 
 size_t workspace(const Desc& d, int pass) {
-    if (pass == MI3D_PASS_FWD) return d.rows ? round256((size_t)d.rows * d.F * d.e) + parts_bytes(plans_of(d, pass).second.splits, d.rows, d.O) : 0;      // h, parts of y
-    if (pass == MI3D_PASS_DGRAD) return d.rows ? parts_bytes(plans_of(d, pass).second.splits, d.rows, d.C) : 0;
-    if (pass != MI3D_PASS_WGRAD) return 0;
+    if (pass < MI3D_PASS_FWD || pass > MI3D_PASS_WGRAD || (!d.rows && pass != MI3D_PASS_WGRAD)) return 0;
     const Plans p = plans_of(d, pass);
+    if (!p.fit()) return 0;
+    if (pass == MI3D_PASS_FWD) return round256((size_t)d.rows * d.F * d.e) + parts_bytes(p.second.splits, d.rows, d.O);      // h, parts of y
+    if (pass == MI3D_PASS_DGRAD) return parts_bytes(p.second.splits, d.rows, d.C);
     const size_t n1 = parts_bytes(p.first.splits, 2 * d.F, d.C), n2 = parts_bytes(p.second.splits, d.O, d.F);
     return p.pair ? n1 + n2 : n1 > n2 ? n1 : n2;
 }
@@ -682,6 +693,7 @@ int mi3d_ffn_kernel_detail(const mi3d_ffn_desc* desc, int pass, char* buf, size_
     if (!buf || !buf_len || pass < MI3D_PASS_FWD || pass > MI3D_PASS_WGRAD) return MI3D_ERR_INVALID_ARG;
     static const char* const names[4] = {"tiles_256x256", "tiles_128x128", "tiles_64x128", "few_rows"};
     const Plans p = plans_of(d, pass);
+    if (!p.fit()) return MI3D_ERR_UNSUPPORTED;
     const char *first = names[p.first.tile], *second = names[p.second.tile];
     if (pass != MI3D_PASS_WGRAD) snprintf(buf, buf_len, "%s, %s parts %d", first, second, p.second.splits);
     else if (p.pair) snprintf(buf, buf_len, "pair %s parts %d", first, p.first.splits);
@@ -696,6 +708,7 @@ int mi3d_ffn_gate(const mi3d_ffn_desc* desc, const void* x, const void* w1, void
     if (!usable(w1) || !aligned16(x) || !aligned16(h) || !aligned16(gu)) return MI3D_ERR_INVALID_ARG;
     if (d.rows == 0) return MI3D_OK;
     if (!x || !h) return MI3D_ERR_INVALID_ARG;
+    if (!plans_of(d, MI3D_PASS_FWD).first.fits()) return MI3D_ERR_UNSUPPORTED;
     return d.e == 2 ? gate<uint16_t>(d, x, w1, h, gu, (hipStream_t)stream) : gate<float>(d, x, w1, h, gu, (hipStream_t)stream);
 }
 
@@ -706,6 +719,7 @@ int mi3d_ffn_fwd(const mi3d_ffn_desc* desc, const void* x, const void* w1, const
     if (!usable(w1) || !usable(w2) || !aligned16(x) || !aligned16(y) || !aligned16(gu) || !aligned16(ws)) return MI3D_ERR_INVALID_ARG;
     if (d.rows == 0) return MI3D_OK;
     if (!x || !y) return MI3D_ERR_INVALID_ARG;
+    if (!plans_of(d, MI3D_PASS_FWD).fit()) return MI3D_ERR_UNSUPPORTED;
     if (!ws || ws_bytes < workspace(d, MI3D_PASS_FWD)) return MI3D_ERR_WORKSPACE;
     const hipStream_t s = (hipStream_t)stream;
     st = d.e == 2 ? gate<uint16_t>(d, x, w1, ws, gu, s) : gate<float>(d, x, w1, ws, gu, s);
@@ -722,6 +736,7 @@ int mi3d_ffn_dgrad(const mi3d_ffn_desc* desc, const void* dy, const void* w1, co
         return MI3D_ERR_INVALID_ARG;
     if (d.rows == 0) return MI3D_OK;
     if (!dy || !gu || !dgu || !h || !dx) return MI3D_ERR_INVALID_ARG;
+    if (!plans_of(d, MI3D_PASS_DGRAD).fit()) return MI3D_ERR_UNSUPPORTED;
     const size_t need = workspace(d, MI3D_PASS_DGRAD);
     if (need && (!ws || ws_bytes < need)) return MI3D_ERR_WORKSPACE;
     return d.e == 2 ? dgrad<uint16_t>(d, dy, w1, w2, gu, dgu, h, dx, ws, (hipStream_t)stream) : dgrad<float>(d, dy, w1, w2, gu, dgu, h, dx, ws, (hipStream_t)stream);
@@ -734,6 +749,7 @@ int mi3d_ffn_wgrad(const mi3d_ffn_desc* desc, const void* x, const void* dgu, co
     if (st) return st;
     if (!usable(dw1) || !usable(dw2) || !aligned16(x) || !aligned16(dgu) || !aligned16(h) || !aligned16(dy) || !aligned16(ws)) return MI3D_ERR_INVALID_ARG;
     if (d.rows && (!x || !dgu || !h || !dy)) return MI3D_ERR_INVALID_ARG;
+    if (!plans_of(d, MI3D_PASS_WGRAD).fit()) return MI3D_ERR_UNSUPPORTED;
     const size_t need = workspace(d, MI3D_PASS_WGRAD);
     if (need && (!ws || ws_bytes < need)) return MI3D_ERR_WORKSPACE;
     const hipStream_t s = (hipStream_t)stream;

@@ -122,7 +122,8 @@ static int blocks_of(long long rows, int N) {
 double few_rows_us(bool bf16, long long rows, long long K, long long N) {
     const int nb = blocks_of(rows, (int)N);
     const double groups = (double)((N + 15) / 16) * (double)((rows + 16 * nb - 1) / (16 * nb)) / cu_count(), pieces = (double)((K * (bf16 ? 2 : 4) + 127) / 128);
-    if ((rows + 16 * nb - 1) / (16 * nb) > 65535) return 1e30;
+    const long long down = (rows + 16 * nb - 1) / (16 * nb), across = (N + 15) / 16;
+    if (down > 65535 || down * across * 512 >= (1ll << 31)) return 1e30;      // (a launch's second dimension, and its threads of 8 waves each)
     static constexpr double each[2][3] = {{0.12, 0.30, 0.60}, {0.09, 0.22, 0.40}};
     return 3.5 + (groups < 1.0 ? 1.0 : groups) * ((bf16 ? 0.2 : 0.8) + pieces * each[bf16][nb / 2]);
 }
