@@ -10,13 +10,14 @@ pytestmark = pytest.mark.gpu
 U = 2.0 ** -24
 HALF = {torch.bfloat16: 2.0 ** -8, torch.float32: 2.0 ** -24}
 TINY = 2.0 ** -122      # (smaller values may be cut to zero on the way)
-DTYPES = [torch.float32]
+DTYPES = [torch.float32, torch.bfloat16]
 
 
 def phi_error(g, dtype):
     """Relative error of Phi(g).  fp32: erfc of a z = -g / sqrt 2 with two roundings, each of which moves it by up to 1 + 2 z^2 = 1 + g^2 of
-    itself, and the function's own 8 units in the last place."""
-    return (2 * (1 + g * g) + 16) * U
+    itself, and the function's own 8 units in the last place.  bf16: that of the approximation (2e-4) and of its exponential, whose
+    argument carries three roundings of up to g^2 / 2, and some twelve units of the products around it."""
+    return (2 * (1 + g * g) + 16) * U if dtype == torch.float32 else 2e-4 + (2 * g * g + 24) * U
 
 
 def gates(dtype):
@@ -36,7 +37,7 @@ def functions(g):
     return c, p
 
 
-@pytest.mark.parametrize("dtype", DTYPES, ids=["f32"])
+@pytest.mark.parametrize("dtype", DTYPES, ids=["f32", "bf16"])
 @pytest.mark.parametrize("rows", [None, 40], ids=["all", "few"])
 def test_forward(device, dtype, rows):
     """u = 1 and g from one product each: [g | u] is exact."""
@@ -55,7 +56,7 @@ def test_forward(device, dtype, rows):
     close(h, ref, 1.01 * ref.abs() * (HALF[dtype] + phi_error(g, dtype) + 4 * U) + TINY, "h")
 
 
-@pytest.mark.parametrize("dtype", DTYPES, ids=["f32"])
+@pytest.mark.parametrize("dtype", DTYPES, ids=["f32", "bf16"])
 def test_data_gradient(device, dtype):
     """dh = 1 and u = 1: [dg | du] is [act' | act]."""
     C, F = 8, 16
