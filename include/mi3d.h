@@ -370,11 +370,13 @@ int mi3d_layernorm_bwd_f32(const void *dy, const void *x, const float *stats, co
 /* Dropout whose mask is drawn again in the backward pass instead of being stored.  Number i of the stream (seed, offset) is
  * half i % 2 (0: low) of word (i % 8) / 2 of Philox 4x32-10 (Salmon et al., SC 2011) for the counter words (i / 8 low,
  * i / 8 high, offset low, offset high) and the key (seed low, seed high).  Value i is kept where number i is below
- * T = 65536 (1 - p) rounded to a whole number, and then multiplied by 65536 / T; p is thus taken to the next multiple of
- * 2^-16.  0 <= p <= 1; p = 1 keeps nothing.  A dropped value is 0 whatever it was (an infinity, a NaN).
+ * T = 65536 (1 - p) rounded to a whole number, and then multiplied by 65536 / T; p is thus taken to the nearest multiple of
+ * 2^-16.  0 <= p <= 1; T = 0 (p = 1, or within 2^-17 of it) keeps nothing.  A dropped value is 0 whatever it was (an infinity, a NaN).
  * offset tells the layers and steps of a run apart: streams of different (seed, offset) share no numbers by design.
  * dev_offset (may be NULL, 8-byte aligned): a number in device memory that is added to offset when the kernel runs, for
- * captured graphs whose replays have to differ.
+ * captured graphs whose replays have to differ.  It is the sum that tells streams apart: the offsets of calls that share a
+ * dev_offset have to be further apart than the number ever grows (layer << 40, say).  With neighbouring offsets and a number
+ * that counts steps, a layer draws the numbers of the next layer one step later.
  *   _fwd       out[i] = residual[i] + dropout(a)[i]; residual may be NULL (0); out may be a or residual.
  *   _bwd       da[i] = dropout(dout)[i] with the same numbers; da may be dout.  (The residual's gradient is dout.)
  *   _channels  whole feature maps: every value of channel c of sample n of a [N][voxels][C] goes by number n * C + c; forward

@@ -204,7 +204,8 @@ def layernorm_bwd(dy, x, stats, gamma, dx=None, dgamma=None, dbeta=None, ws=None
 
 def dropout_fwd(a, p, seed, offset=0, residual=None, out=None, dev_offset=None):
     """out = residual + dropout(a) with the numbers of stream (seed, offset); dev_offset: an int64 of one value on the device that is
-    added to offset when the kernel runs.  out may be a or residual."""
+    added to offset when the kernel runs: calls that share it need offsets further apart than it ever grows (layer << 40, say), or
+    one layer draws in this step what another one drew in an earlier step.  out may be a or residual."""
     fn, (dev, stream) = _typed("mi3d_dropout_fwd", a.dtype), _current(a, "a")
     if out is None:
         out = torch.empty_like(a, memory_format=torch.contiguous_format)
@@ -215,7 +216,8 @@ def dropout_fwd(a, p, seed, offset=0, residual=None, out=None, dev_offset=None):
 
 
 def dropout_bwd(dout, p, seed, offset=0, da=None, dev_offset=None):
-    """da = the gradient of dropout_fwd's a: the same values are dropped.  da may be dout."""
+    """da = the gradient of dropout_fwd's a: the same values are dropped (seed, offset and dev_offset as in the forward pass).  da may be
+    dout."""
     fn, (dev, stream) = _typed("mi3d_dropout_bwd", dout.dtype), _current(dout, "dout")
     if da is None:
         da = torch.empty_like(dout, memory_format=torch.contiguous_format)
@@ -226,7 +228,8 @@ def dropout_bwd(dout, p, seed, offset=0, da=None, dev_offset=None):
 
 
 def dropout_channels(a, p, seed, offset=0, out=None, dev_offset=None):
-    """Drops whole channels of the samples of a [N, ..., C]; forward and backward pass alike.  out may be a."""
+    """Drops whole channels of the samples of a [N, ..., C]; forward and backward pass alike.  dev_offset: as in dropout_fwd.  out may
+    be a."""
     if a.dim() < 2:
         raise ValueError(f"a: need [N, ..., C], got {tuple(a.shape)}")
     fn, (dev, stream) = _typed("mi3d_dropout_channels", a.dtype), _current(a, "a")
