@@ -8,8 +8,14 @@
 // lies, by loads that go to LDS directly, 64 or 128 bytes of k a step: operands with k across are read from there transposed
 // (bf16: ds_read_b64_tr_b16), so that no pass rewrites a tensor or the weights.  P goes into the first operand of the matrix
 // instruction, whose results a lane then holds as four neighbouring n of one row.  bf16: v_mfma_f32_32x32x16_bf16; fp32:
-// v_mfma_f32_32x32x2_f32 on the same 16-byte pieces, four of k.  Sums in fp32.  Tensors between two calls are rounded to their type
-// once (h, [dg | du]), as the convolutions' are.
+// v_mfma_f32_32x32x2_f32 on the same 16-byte pieces, four of k.  Sums in fp32.
+//
+// Rounded to the type on the way, beside the results themselves: h between the two forward products, and [dg | du] before dx is formed
+// from it (dx thus belongs to the [dg | du] that the weight gradient reads).  In bf16 both are operands of instructions that take
+// bf16; in two parts each they would double their product's k, 42 -> 72 us of 131 (forward, 27648 x 320 x 1280) and 237 -> 462 of 483
+// (data gradient, 16384 x 1024 x 4096).  What it costs: an error against 64 bits of 2.3e-3 to 2.4e-3 in the 2-norm, where one rounding at
+// the end has 1.65e-3.  h and the activation's derivative in the data gradient come from the rounded [g | u], the only one that is
+// kept, so dw2 reads an h that is up to a rounding of g and u off the forward pass's.  Whoever needs more takes fp32.
 //
 // Bound: the matrix instructions on long contractions (8192 x 4096 x 8192: 1358 TFLOP/s, where a library product of 8192^3 reaches
 // 1275; fp32, 16384 x 1024 x 4096, 132 to 139, and 130); the results of short ones, which every workgroup has to write (and for the data gradient read [g | u])

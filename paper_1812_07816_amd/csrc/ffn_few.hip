@@ -102,7 +102,7 @@ __global__ void __launch_bounds__(512) few_rows_kernel(const T* __restrict__ x, 
 #pragma unroll
             for (int j = 0; j < 4; ++j) v[0][j] = activation<T, ACT>(v[0][j]) * v[1][j];
         }
-        put(out + (long long)m * N + n, v[0]);
+        put(out + (long long)m * N + n, v[0]);      // (GATED: h, rounded to its type for the second product, as on tiles)
     }
 }
 
