@@ -7,7 +7,7 @@
 // One draw of the generator serves the eight values that a thread moves at a time.
 //
 // Bound: HBM for the values; the generator's ten rounds (20 products of 32 by 32 bits) run beside the loads.  bf16, 192^3 x 32 with a
-// residual: 272 us = 5.0 TB/s (a copy reaches 5.15); whole channels, 2 x 96^3 x 64: 84 us = 5.4 TB/s, out of the last cache in part.
+// residual: 272 us = 5.0 TB/s (a copy reaches 5.1); whole channels, 2 x 96^3 x 64: 84 us = 5.4 TB/s, out of the last cache in part.
 #include <cmath>
 
 #include "mi3d_internal.h"

@@ -17,12 +17,13 @@
 // the end has 1.65e-3.  h and the activation's derivative in the data gradient come from the rounded [g | u], the only one that is
 // kept, so dw2 reads an h that is up to a rounding of g and u off the forward pass's.  Whoever needs more takes fp32.
 //
-// Bound: the matrix instructions on long contractions (8192 x 4096 x 8192: 1358 TFLOP/s, where a library product of 8192^3 reaches
-// 1275; fp32, 16384 x 1024 x 4096, 132 to 139, and 130); the results of short ones, which every workgroup has to write (and for the data gradient read [g | u])
-// before its compute unit goes on: 16384 x 1024 x 4096 data gradient 247 + 228 us, 27648 x 320 x 1280 forward 87 + 41 us.
+// Bound: the matrix instructions on long contractions (dx of 8192 x 4096 x 8192: 913 us, 1204 TFLOP/s, where a library product of 8192^3
+// reaches 1294; fp32, 16384 x 1024 x 4096: 134 to 139, and 131, the data gradient's first product 120); the results of short ones, which
+// every workgroup has to write (and for the data gradient read [g | u]) before its compute unit goes on: 16384 x 1024 x 4096 data gradient
+// 247 + 237 us, 27648 x 320 x 1280 forward 89 + 42 us (three sets of tensors in turn; 228 + 227 and 75 + 43 on one set again and again).
 // Measured on the way (16384 x 1024 x 4096, data gradient): results straight from registers, 8 bytes a lane, 811 us; through LDS 571;
-// without bank conflicts the same; fragments a turn ahead and loads between the products 475; results streamed 443 to 475
-// (by device; the two kernels alone).  Not faster: two to four workgroups of smaller tiles on a unit, deeper rings, workgroups of a unit out of step, wave priorities.
+// without bank conflicts the same; fragments a turn ahead and loads between the products 475; results streamed 10 less (below).  Not
+// faster: two to four workgroups of smaller tiles on a unit, deeper rings, workgroups of a unit out of step, wave priorities.
 
 #include <cstdio>
 
@@ -262,7 +263,8 @@ __device__ __forceinline__ void ffn_tile(const FfnParams& P, const int block) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // (the loads behind the last step)
 
     // (GATE, DACT: what comes and goes here is several times what the operands are, which stay in L2 if it is streamed past them: the two
-    // products of 16384 x 1024 x 4096's data gradient 238 + 233 -> 229 + 214 us.)
+    // products of 16384 x 1024 x 4096's data gradient 238 + 229 -> 228 + 227 us.  h, which the next product reads, goes past L2 as well: 27648 x
+    // 320 x 1280 forward 76 + 40 -> 75 + 43.)
     // The results go through LDS (a lane holds four columns of one row; 16-byte pieces permuted by the row) so that each row's are
     // read and written in whole lines, eight values a thread, RA of the MB blocks of rows at a time.  The data gradient's g and u
     // are requested before.
@@ -442,11 +444,12 @@ int launch_pair(FfnPair P, hipStream_t s) {
 // The time of a product on tiles is rounds of workgroups (one or two on a compute unit), each of which takes a fixed time (first
 // loads, results) and a time for every 128 bytes of k; less where it has its compute unit for itself.  Microseconds, measured over
 // 300 to 27648 rows, 200 to 4096 channels and F 520 to 8192 (LARGE, MIDDLE, SMALL in us):
-//   LARGE  256 x 256, 8 waves: fewest LDS reads a product, but alone on its unit: dx of 16384 x 1024 x 4096 231, 297, 377
+//   LARGE  256 x 256, 8 waves: fewest LDS reads a product, but alone on its unit: dx of 16384 x 1024 x 4096 240, 277, 373
 //   MIDDLE 128 x 128: two on a unit, which cover some of each other's first loads and results, for short contractions:
-//          first product of 27648 x 320 x 1280 90, 82, 115
-//   SMALL  64 x 128: fills the chip with a quarter of the rows: second product of 3456 x 320 x 1280 30, 19, 11
-//   FEW    no LDS (ffn_few.hip): small matrices and few rows: first product of 300 x 200 x 520 SMALL 6.5, FEW 4.2
+//          first product of 27648 x 320 x 1280 87, 75, 102
+//   SMALL  64 x 128: fills the chip with a quarter of the rows: second product of 3456 x 320 x 1280 33, 19, 11
+//   FEW    no LDS (ffn_few.hip): small matrices and few rows: first product of 300 x 200 x 520 SMALL 6.3, FEW 4.4, of one row of
+//          1024 x 4096 9.4 and 5.8
 enum Tile { LARGE, MIDDLE, SMALL, FEW };
 struct TileTimes {
     int bm, bn, threads, per_cu;
@@ -574,8 +577,8 @@ int make(const mi3d_ffn_desc* d, Desc* o) {
     return MI3D_OK;
 }
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
-// The plans of a pass.  pair: both weight gradients in one launch, else one after the other with parts of their own (16384 x 1024 x 4096:
-// 427 us together, 368 apart; 27000 x 256 x 1024: 68 and 76)
+// The plans of a pass.  pair: both weight gradients in one launch, else one after the other with parts of their own (additions of the parts
+// included, 16384 x 1024 x 4096: 432 us together, 404 apart; 27000 x 256 x 1024: 62 and 74)
 struct Plans {
     Plan first, second;
     bool pair;

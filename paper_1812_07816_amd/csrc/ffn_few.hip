@@ -109,7 +109,9 @@ __global__ void __launch_bounds__(512) few_rows_kernel(const T* __restrict__ x, 
 }  // namespace
 
 // Blocks of 16 rows of a workgroup: as many (up to 4) as leave a workgroup for every compute unit
-// (64 x 4096 -> 1024: 20.5 us with 4, 9.2 with 1; 1331 x 200 -> 2 x 520: 7.9 and 9.6)
+// (64 x 4096 -> 1024: 20.1 us with 4, 13.2 with 2, 9.4 with 1; fp32, 1331 x 200 -> 2 x 520: 17.0, 19.2 and 24.8).  Fewer than 16 x 256 columns
+// of one block of rows leave units idle all the same, as no workgroup takes a part of k: one row of 4096 -> 1024, 64 workgroups, takes 7.1 us for
+// 8.4 MB, 1024 -> 2 x 4096, 256 workgroups, 6.5 us for 16.8 MB.
 static int blocks_of(long long rows, int N) {
     const long long cols = (N + 15) / 16;
     int nb = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
@@ -117,7 +119,8 @@ static int blocks_of(long long rows, int N) {
     return nb;
 }
 
-// What it is expected to take, in microseconds: for every workgroup of a compute unit a fixed time and one for each 128 bytes of k, measured
+// What it is expected to take, in microseconds: for every workgroup of a compute unit (one where there are fewer workgroups than units) a
+// fixed time and one for each 128 bytes of k, measured
 // with 1, 2 and 4 blocks of rows on the sizes above and one row of 1024 and 4096
 double few_rows_us(bool bf16, long long rows, long long K, long long N) {
     const int nb = blocks_of(rows, (int)N);

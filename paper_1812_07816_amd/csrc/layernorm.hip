@@ -3,9 +3,9 @@
 // Backward, from x and the row's (mean, rstd), with g = dy * gamma:
 //   dx = rstd * (g - mean_c(g) - xhat * mean_c(g * xhat)) (+ add),  dgamma = sum_rows dy * xhat,  dbeta = sum_rows dy.
 //
-// Bound: HBM (bf16, 192^3 rows of 32: forward 185 us, backward with a second gradient 345 us = 5.25 TB/s of
-// the tensors alone, 5.4 with the rows' statistics, where a copy reaches 5.15; 27648
-// rows of 320: 10 and 23 us).  A row stays in the registers of L lanes, K pieces of eight values each, so that it is read once and the
+// Bound: HBM (bf16, 192^3 rows of 32: forward 189 us, backward with a second gradient 345 us = 5.25 TB/s of
+// the tensors alone, 5.4 with the rows' statistics, where a copy reaches 5.1; 27648
+// rows of 320: backward 20 us and 4 for the sums, fp32 31 and 5).  A row stays in the registers of L lanes, K pieces of eight values each, so that it is read once and the
 // variance is a sum of squared differences from the mean (no cancellation where the mean is large); sums in fp32.  The
 // sums over rows are kept per lane (a lane always has the same channels), added over the lanes of a workgroup in lane
 // order, and over the workgroups in double in a fixed order by a second launch (bit-reproducible).  fp32 carries 108 rows of a lane and 64
@@ -187,7 +187,7 @@ __global__ void __launch_bounds__(512) ln_bwd_kernel(const T* dy, const T* x, co
 }
 
 // dgamma, dbeta from the workgroups' sums: 16 columns a workgroup, thread (slice, column) adds parts slice, slice + 64, ... in double, and the
-// slices are added in order.  Bound: the latency of the loads, of which four are under way (27648 x 320, 864 parts: 25 us with 16
+// slices are added in order.  Bound: the latency of the loads, of which four are under way (27648 x 320, 864 parts: 4 us; 25 with 16
 // slices and one load at a time).
 __global__ void __launch_bounds__(1024) ln_finish_kernel(const float* __restrict__ part, int parts, int C, float* __restrict__ dgamma, float* __restrict__ dbeta) {
     __shared__ double red[64][17];
@@ -213,7 +213,16 @@ __global__ void __launch_bounds__(1024) ln_finish_kernel(const float* __restrict
 }
 
 // Lanes of a row (a power of two) and pieces of a lane, at most 4: of the ways that fit, the one with the fewest idle lanes, and of
-// those the one with the most lanes; more than a wavefront's only where its lanes cannot hold the row.
+// those the one with the most lanes; more than a wavefront's only where its lanes cannot hold the row.  Measured on 2^27 values,
+// forward / backward in us, where a copy's rate makes 104 / 156 in bf16 and 208 / 313 in fp32:
+//   channels (pieces)   lanes x pieces of a lane: bf16, fp32
+//     56 (7)     8 x 1: 106 / 153, 222 / 301     4 x 2: 123 / 171, 279 / 395     2 x 4: 144 / 204, 353 / 470
+//    200 (25)   32 x 1: 106 / 164, 231 / 307    16 x 2: 112 / 162, 234 / 344     8 x 4: 136 / 204, 253 / 345
+//    320 (40)   16 x 3: 129 / 201, 202 / 339    32 x 2: 129 / 169, 212 / 311    64 x 1: 126 / 204, 230 / 290
+//     24 (3)     1 x 3: 134 / 193, 355 / 506     2 x 2: 126 / 178, 295 / 424     4 x 1: 109 / 158, 227 / 311
+//     72 (9)     4 x 3: 123 / 184, 297 / 442     8 x 2: 125 / 178, 242 / 351    16 x 1: 123 / 195, 236 / 306
+// The rule takes the first of each line.  It is right where a lane then has one piece; rows of 3, 5, 6, 9 or 10 pieces are read in
+// pieces of 16 or 32 bytes out of every 48 to 96, which costs more than idle lanes, most of all in fp32.
 struct Rows {
     Form form;
     int L, K;
@@ -231,7 +240,8 @@ bool rows_plan(int C, Rows* p) {
 }
 int threads_of(const Rows& p) { return p.L > 256 ? p.L : 256; }
 // Workgroups of the backward pass: four for a compute unit, fewer of wide rows, whose registers leave room for two or one and whose sums
-// are a part of the traffic; all with as many turns, but for one (8192 x 4096: 69 us with one, 4096 x 16384: 154 us with four)
+// are a part of the traffic; all with as many turns, but for one.  us with four, two and one, the second launch included (bf16): 8192 x 4096
+// 61, 50, 70; 4096 x 16384 161, 121, 109; 27648 x 320 24, 21, 26 (few turns each: two would do there)
 int parts_of(const Rows& p, size_t rows, int C) {
     const long long most = C <= 1024 ? 1024 : C <= 8192 ? 512 : 256;
     const long long per = threads_of(p) / p.L, turns = ((long long)rows + per - 1) / per, each = (turns + most - 1) / most;
